@@ -41,6 +41,7 @@
 // tiles on an XCD: 148 us.
 // Output layout of the 32x32 MFMA: register r of lane l holds row
 // 8(r/4) + 4(l/32) + r%4, column l%32.
+#include "attention_device.h"
 #include "gemm_device.h"
 #include "p4q_internal.h"
 
@@ -49,15 +50,6 @@
 
 namespace p4q {
 namespace {
-
-typedef _Float16 v8h __attribute__((ext_vector_type(8)));
-typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
-typedef _Float16 v2h __attribute__((ext_vector_type(2)));
-typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
-typedef float v2f __attribute__((ext_vector_type(2)));
-typedef float v16f __attribute__((ext_vector_type(16)));
-typedef short v4s __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) v4s *lds_v4s_t;
 
 constexpr int kD = 128;                 // head dimension
 constexpr int kNW = 4;                  // wavefronts per work-group
@@ -74,33 +66,6 @@ constexpr float kRescale = 8.0f;        // raise the running max past this margi
 // four keys of a transposing read (64-byte pieces) fall in distinct banks.
 __device__ __forceinline__ int k_slot(int r, int c) { return c ^ (r & 15); }
 __device__ __forceinline__ int v_slot(int r, int c) { return c ^ ((r & 3) << 2); }
-
-template <bool BF16>
-__device__ __forceinline__ v16f mfma(uint4 a, uint4 b, v16f c) {
-    if constexpr (BF16)
-        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
-    else
-        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
-}
-
-// two fp32 -> two 16-bit values (nearest, ties to even), low half first
-template <bool BF16>
-__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
-    if constexpr (BF16) return __builtin_bit_cast(uint32_t, __builtin_convertvector(v2f{lo, hi}, v2bf));
-    else return __builtin_bit_cast(uint32_t, __builtin_convertvector(v2f{lo, hi}, v2h));
-}
-
-// the same of lo * c and hi * c.  In fp16 the product is rounded once, straight
-// to 16 bits (v_fma_mixlo_f16), which takes a conversion of its own for each: the
-// packed one is handed products that are already rounded to fp32.
-template <bool BF16>
-__device__ __forceinline__ uint32_t pack2_scaled(float lo, float hi, float c) {
-    if constexpr (BF16) return pack2<true>(lo * c, hi * c);
-    else {
-        const _Float16 a = (_Float16)(lo * c), b = (_Float16)(hi * c);
-        return (uint32_t)__builtin_bit_cast(uint16_t, a) | ((uint32_t)__builtin_bit_cast(uint16_t, b) << 16);
-    }
-}
 
 template <bool BF16, bool CAUSAL>
 __global__ __launch_bounds__(64 * kNW, 2) void k_attention(const uint16_t *__restrict__ q,
@@ -175,16 +140,6 @@ __global__ __launch_bounds__(64 * kNW, 2) void k_attention(const uint16_t *__res
     for (int db = 0; db < 4; ++db) acc[db] = v16f{};
     float m = -__builtin_huge_valf(), lsum = 0.0f;
 
-    // lanes l and l ^ 32 hold the two halves of a query's keys: their
-    // combination through a permlane swap (no LDS round trip)
-    auto xmax32 = [](float x) __attribute__((always_inline)) {
-        const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-        return __builtin_fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
-    };
-    auto xsum32 = [](float x) __attribute__((always_inline)) {
-        const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-        return __uint_as_float(p[0]) + __uint_as_float(p[1]);
-    };
     // K fragment addresses: row 32 hf + c32 (its k_slot depends on c32 only)
     const uint32_t kofs = (uint32_t)(c32 * kRow);
     const uint32_t kx = (uint32_t)(c32 & 15);
