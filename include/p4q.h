@@ -239,6 +239,110 @@ int p4q_attention_prefill(p4q_dtype dt, int B, int L, int H, int D,
                           void *out, int64_t ld_out, int causal, hipStream_t stream);
 
 /* ------------------------------------------------------------------------
+ * Serving the pruned prompt: a paged key-value cache and the attention that
+ * reads it (Appendix B.3: key and value caches in 16 bits).
+ *
+ * The cache.  k_cache and v_cache are [num_pages, Hk, page_size, D] of dt,
+ * page_size a power of two from 16 to 4096.  Row b of block_table int32
+ * [B, max_pages] lists the pages of sequence b in order: its key s is row
+ * s % page_size of page block_table[b][s / page_size], for every key head.
+ * Entries past a sequence's keys are not read.  Sequences may share pages
+ * that no call appends to.
+ *
+ * Packed rows.  cu_seqlens int32 [B + 1], ascending from 0: sequence b has
+ * rows cu_seqlens[b] .. cu_seqlens[b + 1] - 1 (none is allowed).  Rows from
+ * cu_seqlens[B] on (a padded batch) are neither used nor written.
+ *
+ * Heads.  Hq query heads, Hk key heads, Hq % Hk == 0: query head h reads key
+ * head h / (Hq / Hk).  Head h of a row starts at column h D.  D is 64 or 128.
+ *
+ * Lengths, tables and positions live on the device and are not known on the
+ * host, so what they hold cannot be refused.  Values out of range read and write
+ * nothing out of range: a token whose place has no page in the cache is not
+ * appended, and a query that sees a key without one (an entry outside
+ * [0, num_pages), a length past the table or past max_len) gets NaN.
+ * Negative lengths count as 0.  cu_seqlens that do not ascend, or that leave the
+ * rows, are cut to them.
+ *
+ * p4q_rope_append: token t, the i-th of sequence b in this call, takes place
+ * s = cache_lens[b] + i in its sequence (cache_lens int32 [B]: keys cached
+ * before the call; NULL: 0) and rotates by p = positions[t] (int32 [T]: pruned
+ * tokens may keep the positions of the unpruned prompt; NULL: p = s):
+ *   x'[j]       = x[j] cos(p theta_j) - x[j + D/2] sin(p theta_j)
+ *   x'[j + D/2] = x[j + D/2] cos(p theta_j) + x[j] sin(p theta_j),  j < D/2,
+ *   theta_j = rope_base^(-2j/D),
+ * for x every query head (to q_out) and every key head (to the cache and, unless
+ * it is NULL, to k_out); v goes to the cache as it is.  fp32 arithmetic on
+ * 64-bit angles, each result rounded once.  q_out may be q and k_out may be k
+ * (same pointer and row stride); other overlaps are not allowed, nor may two
+ * tokens of a call take the same row of the cache.
+ *
+ * p4q_attention_packed: sequence b has n = cu_seqlens[b + 1] - cu_seqlens[b]
+ * tokens and m keys, by cu_seqlens_k in the same way (NULL: cu_seqlens).  Its
+ * token i, head h:
+ *   S[j] = <q[i, h], k[j, h / (Hq / Hk)]> / sqrt(D),
+ *     over j <= i + m - n (causal = 1: the last token sees the last key)
+ *     or every j < m (causal = 0),
+ *   out[i, h] = sum_j softmax_j(S) v[j, h / (Hq / Hk)];  zeros without a key.
+ * Arithmetic as p4q_attention_prefill.  A non-finite value row may also reach
+ * tokens whose mask ends less than 32 keys before it.
+ *
+ * p4q_attention_prefill_paged: the same with the m = seq_lens[b] keys of the
+ * cache (int32 [B]; the call's own tokens included, appended before).
+ *
+ * p4q_attention_decode: one query row per sequence, over its seq_lens[b] keys
+ * (its own included; none: zeros).  max_len, a bound of seq_lens, at most
+ * max_pages * page_size, decides how the keys are split among work-groups.
+ *
+ * Layouts: q [T, ldq] (decode: [B, ldq]), k and v [T (packed: Tk), ldk / ldv],
+ *   out [T (B), ld_out], q_out and k_out alike, all of dt; rows may be columns
+ *   of a wider (fused q|k|v) buffer.
+ * Workspaces: p4q_attention_prompt_workspace_bytes (for both prompt calls;
+ *   most_keys bounds the keys of a sequence: Tk, or max_pages * page_size) is
+ *   nonzero where few rows meet many keys; given that much (16-byte aligned)
+ *   the call splits the keys of a row among work-groups, without it the call
+ *   runs unsplit, and the two agree within the rounding of fp32 sums.  Nothing
+ *   of it is read before the call has written it.
+ *   p4q_attention_decode_workspace_bytes: required where nonzero, 16-byte
+ *   aligned; its first 32768 bytes hold arrival counters, which must be zero
+ *   before the first call and are zero again after each.  Calls that share a
+ *   workspace must not overlap.  Both sizes depend on the current device.
+ *   A sequence's result does not depend on the order in which its parts finish.
+ * Limits: T, B >= 1, T <= 2^24, B <= 65535, Tk >= 0, Hq <= 1024, T Hq / Hk <
+ *   2^31, max_pages * page_size < 2^30; row strides >= heads * D, multiples of 8
+ *   and < 2^24; rope_base > 1; data pointers 16-byte aligned, int32 pointers
+ *   4-byte aligned.
+ * ---------------------------------------------------------------------- */
+int p4q_rope_append(p4q_dtype dt, int T, int B, int Hq, int Hk, int D, const void *q, int64_t ldq,
+                    const void *k, int64_t ldk, const void *v, int64_t ldv,
+                    const int32_t *cu_seqlens, const int32_t *cache_lens,
+                    const int32_t *positions, float rope_base, void *q_out, int64_t ldq_out,
+                    void *k_out, int64_t ldk_out, void *k_cache, void *v_cache, int num_pages,
+                    int page_size, const int32_t *block_table, int max_pages, hipStream_t stream);
+
+size_t p4q_attention_prompt_workspace_bytes(int T, int B, int Hq, int Hk, int D, int64_t most_keys);
+
+int p4q_attention_packed(p4q_dtype dt, int T, int Tk, int B, int Hq, int Hk, int D, const void *q,
+                         int64_t ldq, const void *k, int64_t ldk, const void *v, int64_t ldv,
+                         const int32_t *cu_seqlens, const int32_t *cu_seqlens_k, void *out,
+                         int64_t ld_out, int causal, void *ws, size_t ws_bytes, hipStream_t stream);
+
+int p4q_attention_prefill_paged(p4q_dtype dt, int T, int B, int Hq, int Hk, int D, const void *q,
+                                int64_t ldq, const void *k_cache, const void *v_cache, int num_pages,
+                                int page_size, const int32_t *block_table, int max_pages,
+                                const int32_t *cu_seqlens, const int32_t *seq_lens, void *out,
+                                int64_t ld_out, int causal, void *ws, size_t ws_bytes,
+                                hipStream_t stream);
+
+size_t p4q_attention_decode_workspace_bytes(int B, int Hq, int Hk, int D, int max_len);
+
+int p4q_attention_decode(p4q_dtype dt, int B, int Hq, int Hk, int D, const void *q, int64_t ldq,
+                         const void *k_cache, const void *v_cache, int num_pages, int page_size,
+                         const int32_t *block_table, int max_pages, const int32_t *seq_lens,
+                         int max_len, void *out, int64_t ld_out, void *ws, size_t ws_bytes,
+                         hipStream_t stream);
+
+/* ------------------------------------------------------------------------
  * Channel-scaled per-row quantizer (Sec. 3.3 and Appendix B.3: the diagonal
  * channel scales and clipping factors that calibration learns, applied
  * before RTN; also the folded-weight quantization after calibration).

@@ -427,6 +427,53 @@ def attention_prefill(q: np.ndarray, k: np.ndarray, v: np.ndarray, causal: bool 
 
 
 # --------------------------------------------------------------------------
+# O8: serving -- rotary positions, the paged cache, attention of grouped heads
+# --------------------------------------------------------------------------
+def rope(x: np.ndarray, positions: np.ndarray, base: float = 10000.0) -> np.ndarray:
+    """Rotate x [T, H, D] (real numbers) by its positions [T]: channel j < D/2 is
+    paired with j + D/2 and turned by p base^(-2j/D), all in float64."""
+    D = x.shape[-1]
+    theta = float(base) ** (-2.0 * np.arange(D // 2) / D)
+    angle = np.asarray(positions, dtype=np.float64)[:, None] * theta
+    c, s = np.cos(angle)[:, None, :], np.sin(angle)[:, None, :]
+    a, b = x[..., :D // 2].astype(np.float64), x[..., D // 2:].astype(np.float64)
+    return np.concatenate([a * c - b * s, b * c + a * s], axis=-1)
+
+
+def cache_rows(cache: np.ndarray, table_row: np.ndarray, m: int) -> np.ndarray:
+    """The first m keys [m, Hk, D] of a sequence whose pages table_row lists, in a
+    cache [pages, Hk, P, D]."""
+    P = cache.shape[2]
+    return np.stack([cache[table_row[s // P], :, s % P] for s in range(m)]) if m else cache[:0, :, 0]
+
+
+def grouped_attention(q: np.ndarray, k: np.ndarray, v: np.ndarray, causal: bool = True):
+    """Attention of n tokens q [n, Hq, D] over m keys k, v [m, Hk, D] (real
+    numbers), query head h reading key head h / (Hq / Hk).  Causal: token i sees
+    keys j <= i + m - n.  Tokens that see no key give zeros.
+
+    Returns (O, A), float64 [n, Hq, D]: the outputs, and sum_j P_j |v_j|, the scale
+    of what rounding the weights P may move."""
+    n, Hq, D = q.shape
+    m, Hk, _ = k.shape
+    O, A = np.zeros((n, Hq, D)), np.zeros((n, Hq, D))
+    if n == 0 or m == 0:
+        return O, A
+    allowed = np.ones((n, m), dtype=bool)
+    if causal:
+        allowed = np.arange(m)[None, :] <= np.arange(n)[:, None] + (m - n)
+    some = allowed.any(axis=1)
+    for h in range(Hq):
+        kh, vh = (x[:, h // (Hq // Hk)].astype(np.float64) for x in (k, v))
+        S = (q[:, h].astype(np.float64) @ kh.T) / np.sqrt(D)
+        S = np.where(allowed, S, -np.inf)[some]
+        P = np.exp(S - S.max(axis=1, keepdims=True))
+        P = P / P.sum(axis=1, keepdims=True)
+        O[some, h], A[some, h] = P @ vh, P @ np.abs(vh)
+    return O, A
+
+
+# --------------------------------------------------------------------------
 # O4: the W4A4 linear (integer GEMM on codes + dequant epilogue)
 # --------------------------------------------------------------------------
 def int_gemm(a_codes: np.ndarray, w_codes: np.ndarray) -> np.ndarray:

@@ -41,6 +41,20 @@ SIGNATURES = {
                                    _vp, _vp, _vp]),
     "p4q_attention_prefill": (_c_int, [_c_int, _c_int, _c_int, _c_int, _c_int, _vp, _vp, _vp,
                                        _c_i64, _vp, _c_i64, _c_int, _vp]),
+    "p4q_rope_append": (_c_int, [_c_int, _c_int, _c_int, _c_int, _c_int, _c_int, _vp, _c_i64, _vp,
+                                 _c_i64, _vp, _c_i64, _vp, _vp, _vp, _c_float, _vp, _c_i64, _vp,
+                                 _c_i64, _vp, _vp, _c_int, _c_int, _vp, _c_int, _vp]),
+    "p4q_attention_prompt_workspace_bytes": (_c_size, [_c_int, _c_int, _c_int, _c_int, _c_int, _c_i64]),
+    "p4q_attention_packed": (_c_int, [_c_int, _c_int, _c_int, _c_int, _c_int, _c_int, _c_int, _vp,
+                                      _c_i64, _vp, _c_i64, _vp, _c_i64, _vp, _vp, _vp, _c_i64,
+                                      _c_int, _vp, _c_size, _vp]),
+    "p4q_attention_prefill_paged": (_c_int, [_c_int, _c_int, _c_int, _c_int, _c_int, _c_int, _vp,
+                                             _c_i64, _vp, _vp, _c_int, _c_int, _vp, _c_int, _vp, _vp,
+                                             _vp, _c_i64, _c_int, _vp, _c_size, _vp]),
+    "p4q_attention_decode_workspace_bytes": (_c_size, [_c_int, _c_int, _c_int, _c_int, _c_int]),
+    "p4q_attention_decode": (_c_int, [_c_int, _c_int, _c_int, _c_int, _c_int, _vp, _c_i64, _vp, _vp,
+                                      _c_int, _c_int, _vp, _c_int, _vp, _c_int, _vp, _c_i64, _vp,
+                                      _c_size, _vp]),
     "p4q_quant_scaled": (_c_int, [_c_int, _c_int, _c_int, _vp, _c_i64, _vp, _c_int, _c_float, _vp,
                                   _vp, _vp, _vp, _vp, _vp]),
     "p4q_calib_linear_workspace_bytes": (_c_size, [_c_int, _c_int, _c_int]),

@@ -293,6 +293,213 @@ def attention_prefill(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, B: int,
     return out
 
 
+# --------------------------------------------------------------------------- serving
+def _rows_of(t: torch.Tensor, name: str, rows: Optional[int], cols: int, dtype) -> None:
+    """A 2-D operand [rows, >= cols] whose rows may be columns of a wider buffer."""
+    if t.dim() != 2 or t.shape[1] < cols or (rows is not None and t.shape[0] != rows):
+        raise ValueError(f"{name} must have shape ({'rows' if rows is None else rows}, >= {cols}), got {tuple(t.shape)}")
+    if t.stride(1) != 1:
+        raise ValueError(f"{name} must have unit column stride")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+
+
+def _ld(t: torch.Tensor, cols: int) -> int:
+    """Row stride of a 2-D operand (one row may have any: its own width then)."""
+    return t.stride(0) if t.shape[0] > 1 else max(cols, t.stride(0)) // 8 * 8
+
+
+def _ints(t: Optional[torch.Tensor], name: str, n: int) -> None:
+    if t is not None and (t.shape != (n,) or t.dtype != torch.int32 or not t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous int32 tensor of shape ({n},), got {t.dtype} {tuple(t.shape)}")
+
+
+def _cache_shape(k_cache: torch.Tensor, v_cache: torch.Tensor, block_table: torch.Tensor, q: torch.Tensor, Hq: int):
+    """(pages, Hk, page size, D, B, table width) of a paged cache and its table."""
+    if q.dtype not in _F16:
+        raise ValueError(f"q must be fp16 or bf16, got {q.dtype}")
+    if k_cache.dim() != 4 or k_cache.shape != v_cache.shape:
+        raise ValueError("k_cache and v_cache must share a shape [pages, Hk, page size, D]")
+    if k_cache.dtype != q.dtype or v_cache.dtype != q.dtype:
+        raise ValueError("the caches must have q's dtype")
+    if not k_cache.is_contiguous() or not v_cache.is_contiguous():
+        raise ValueError("k_cache and v_cache must be contiguous")
+    if block_table.dim() != 2 or block_table.dtype != torch.int32 or not block_table.is_contiguous():
+        raise ValueError("block_table must be a contiguous int32 [B, max_pages] tensor")
+    pages, Hk, page, D = k_cache.shape
+    if Hk < 1 or Hq < 1 or Hq % Hk:
+        raise ValueError(f"Hq = {Hq} is not a multiple of the cache's {Hk} key heads")
+    return pages, Hk, page, D, block_table.shape[0], block_table.shape[1]
+
+
+def rope_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqlens: torch.Tensor,
+                block_table: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, Hq: int,
+                cache_lens: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
+                rope_base: float = 10000.0, q_out: Optional[torch.Tensor] = None,
+                k_out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """Rotate q and k by their positions and append k and v to a paged cache
+    (p4q_rope_append).
+
+    q [T, >= Hq*D], k and v [T, >= Hk*D] (e.g. column slices of one fused q|k|v
+    output), sequences packed by cu_seqlens int32 [B + 1]; caches [pages, Hk,
+    page size, D]; block_table int32 [B, max_pages]; cache_lens int32 [B] (keys
+    cached before; default 0); positions int32 [T] (default: the place in the
+    sequence).  Returns (q_out, k_out): the rotated rows, k's only into a given
+    k_out.  q_out may be q, k_out may be k.  Rows behind the last sequence are
+    left as they were."""
+    pages, Hk, page, D, B, width = _cache_shape(k_cache, v_cache, block_table, q, Hq)
+    T = q.shape[0]
+    _rows_of(q, "q", None, Hq * D, q.dtype)
+    _rows_of(k, "k", T, Hk * D, q.dtype)
+    _rows_of(v, "v", T, Hk * D, q.dtype)
+    _ints(cu_seqlens, "cu_seqlens", B + 1)
+    _ints(cache_lens, "cache_lens", B)
+    _ints(positions, "positions", T)
+    if q_out is not None:
+        _rows_of(q_out, "q_out", T, Hq * D, q.dtype)
+    if k_out is not None:
+        _rows_of(k_out, "k_out", T, Hk * D, q.dtype)
+    _need_gpu(q, k, v, cu_seqlens, block_table, k_cache, v_cache, cache_lens, positions, q_out, k_out)
+    with torch.cuda.device(q.device):
+        if q_out is None:
+            q_out = torch.empty((T, Hq * D), dtype=q.dtype, device=q.device)
+        check(lib().p4q_rope_append(
+            _dtype_code(q.dtype), T, B, Hq, Hk, D, _ptr(q), _ld(q, Hq * D), _ptr(k), _ld(k, Hk * D), _ptr(v),
+            _ld(v, Hk * D), _ptr(cu_seqlens), _ptr(cache_lens), _ptr(positions), rope_base, _ptr(q_out),
+            _ld(q_out, Hq * D), _ptr(k_out), 0 if k_out is None else _ld(k_out, Hk * D), _ptr(k_cache),
+            _ptr(v_cache), pages, page, _ptr(block_table), width, _stream(q.device)))
+    return q_out, k_out
+
+
+def attention_prompt_workspace(T: int, B: int, Hq: int, Hk: int, D: int, most_keys: int,
+                               device) -> Optional[torch.Tensor]:
+    """Workspace for attention_packed() (most_keys: rows of k) and
+    attention_prefill_paged() (most_keys: keys that a row of the table can
+    hold), or None where the call splits nothing.  Its contents do not matter."""
+    with torch.cuda.device(device):
+        n = lib().p4q_attention_prompt_workspace_bytes(T, B, Hq, Hk, D, most_keys)
+        return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+
+
+def _own_prompt_workspace(T, B, Hq, Hk, D, most_keys, device) -> Optional[torch.Tensor]:
+    """Workspace of one call that was given none; a device without room for it
+    runs the call unsplit."""
+    try:
+        return attention_prompt_workspace(T, B, Hq, Hk, D, most_keys, device)
+    except torch.OutOfMemoryError:
+        return None
+
+
+def attention_packed(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqlens: torch.Tensor, Hq: int, Hk: int,
+                     D: int = 128, causal: bool = True, cu_seqlens_k: Optional[torch.Tensor] = None,
+                     out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of packed prompts of different lengths, grouped heads
+    (p4q_attention_packed): q [T, >= Hq*D], k and v [Tk, >= Hk*D] (rows may be
+    columns of a fused q|k|v buffer), cu_seqlens int32 [B + 1], cu_seqlens_k
+    likewise for the keys (default: cu_seqlens).  Causal: a sequence's last token
+    sees its last key.  Returns out [T, Hq*D]; tokens that see no key get zeros,
+    rows behind the last sequence are left as they were."""
+    if q.dtype not in _F16:
+        raise ValueError(f"q must be fp16 or bf16, got {q.dtype}")
+    T, Tk = q.shape[0], k.shape[0]
+    _rows_of(q, "q", None, Hq * D, q.dtype)
+    _rows_of(k, "k", None, Hk * D, q.dtype)
+    _rows_of(v, "v", Tk, Hk * D, q.dtype)
+    if cu_seqlens.dim() != 1 or cu_seqlens.shape[0] < 2:
+        raise ValueError(f"cu_seqlens must have shape (B + 1,), got {tuple(cu_seqlens.shape)}")
+    B = cu_seqlens.shape[0] - 1
+    _ints(cu_seqlens, "cu_seqlens", B + 1)
+    _ints(cu_seqlens_k, "cu_seqlens_k", B + 1)
+    if cu_seqlens_k is None and Tk != T:
+        raise ValueError(f"k has {Tk} rows and q {T}: cu_seqlens_k is needed")
+    if out is not None:
+        _rows_of(out, "out", T, Hq * D, q.dtype)
+    _check(workspace, "workspace", None, torch.uint8)
+    _need_gpu(q, k, v, cu_seqlens, cu_seqlens_k, out, workspace)
+    with torch.cuda.device(q.device):
+        if out is None:
+            out = torch.empty((T, Hq * D), dtype=q.dtype, device=q.device)
+        if workspace is None:
+            workspace = _own_prompt_workspace(T, B, Hq, Hk, D, Tk, q.device)
+        check(lib().p4q_attention_packed(
+            _dtype_code(q.dtype), T, Tk, B, Hq, Hk, D, _ptr(q), _ld(q, Hq * D), _ptr(k), _ld(k, Hk * D), _ptr(v),
+            _ld(v, Hk * D), _ptr(cu_seqlens), _ptr(cu_seqlens_k), _ptr(out), _ld(out, Hq * D), int(causal),
+            _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream(q.device)))
+    return out
+
+
+def attention_prefill_paged(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, cu_seqlens: torch.Tensor,
+                            block_table: torch.Tensor, seq_lens: torch.Tensor, Hq: int, causal: bool = True,
+                            out: Optional[torch.Tensor] = None,
+                            workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of packed tokens over a paged cache (p4q_attention_prefill_paged):
+    a prompt, a chunk of one or a further turn, whose own keys rope_append() has
+    put there.  q [T, >= Hq*D], cu_seqlens int32 [B + 1], seq_lens int32 [B] (keys
+    of each sequence, its tokens of this call included); the rest as
+    attention_packed() and rope_append()."""
+    pages, Hk, page, D, B, width = _cache_shape(k_cache, v_cache, block_table, q, Hq)
+    T = q.shape[0]
+    _rows_of(q, "q", None, Hq * D, q.dtype)
+    _ints(cu_seqlens, "cu_seqlens", B + 1)
+    _ints(seq_lens, "seq_lens", B)
+    if out is not None:
+        _rows_of(out, "out", T, Hq * D, q.dtype)
+    _check(workspace, "workspace", None, torch.uint8)
+    _need_gpu(q, k_cache, v_cache, cu_seqlens, block_table, seq_lens, out, workspace)
+    with torch.cuda.device(q.device):
+        if out is None:
+            out = torch.empty((T, Hq * D), dtype=q.dtype, device=q.device)
+        if workspace is None:
+            workspace = _own_prompt_workspace(T, B, Hq, Hk, D, width * page, q.device)
+        check(lib().p4q_attention_prefill_paged(
+            _dtype_code(q.dtype), T, B, Hq, Hk, D, _ptr(q), _ld(q, Hq * D), _ptr(k_cache), _ptr(v_cache), pages,
+            page, _ptr(block_table), width, _ptr(cu_seqlens), _ptr(seq_lens), _ptr(out), _ld(out, Hq * D),
+            int(causal), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream(q.device)))
+    return out
+
+
+def attention_decode_workspace(B: int, Hq: int, Hk: int, D: int, max_len: int, device) -> Optional[torch.Tensor]:
+    """Workspace for attention_decode(), or None where it needs none.  Its head
+    holds arrival counters that start at zero (every call leaves them zero again)."""
+    with torch.cuda.device(device):
+        n = lib().p4q_attention_decode_workspace_bytes(B, Hq, Hk, D, max_len)
+        if n == 0:
+            return None
+        ws = torch.empty(n, dtype=torch.uint8, device=device)
+        ws[:32768].zero_()
+        return ws
+
+
+def attention_decode(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, block_table: torch.Tensor,
+                     seq_lens: torch.Tensor, Hq: int, max_len: Optional[int] = None,
+                     out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of one new token per sequence over a paged cache
+    (p4q_attention_decode): q [B, >= Hq*D], seq_lens int32 [B] (keys of each
+    sequence, the new one included; 0: zeros), max_len a bound of them (default:
+    what a row of block_table holds).  Without `workspace` the call makes one if it
+    needs one; a given one must come from attention_decode_workspace() and serve one
+    call at a time.  Returns out [B, Hq*D]."""
+    pages, Hk, page, D, B, width = _cache_shape(k_cache, v_cache, block_table, q, Hq)
+    _rows_of(q, "q", B, Hq * D, q.dtype)
+    _ints(seq_lens, "seq_lens", B)
+    if out is not None:
+        _rows_of(out, "out", B, Hq * D, q.dtype)
+    _check(workspace, "workspace", None, torch.uint8)
+    _need_gpu(q, k_cache, v_cache, block_table, seq_lens, out, workspace)
+    if max_len is None:
+        max_len = width * page
+    with torch.cuda.device(q.device):
+        if out is None:
+            out = torch.empty((B, Hq * D), dtype=q.dtype, device=q.device)
+        if workspace is None:
+            workspace = attention_decode_workspace(B, Hq, Hk, D, max_len, q.device)
+        check(lib().p4q_attention_decode(
+            _dtype_code(q.dtype), B, Hq, Hk, D, _ptr(q), _ld(q, Hq * D), _ptr(k_cache), _ptr(v_cache), pages, page,
+            _ptr(block_table), width, _ptr(seq_lens), max_len, _ptr(out), _ld(out, Hq * D), _ptr(workspace),
+            0 if workspace is None else workspace.numel(), _stream(q.device)))
+    return out
+
+
 # --------------------------------------------------------------------------- calibration
 def quant_scaled(z: torch.Tensor, sigma: torch.Tensor, divide: bool, clip: float = 1.0,
                  clip_rows: Optional[torch.Tensor] = None):

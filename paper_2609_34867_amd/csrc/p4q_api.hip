@@ -5,6 +5,7 @@
 #include <cstdio>
 #include <cstring>
 
+#include "kv_cache.h"
 #include "p4q_internal.h"
 
 namespace {
@@ -281,6 +282,170 @@ int p4q_attention_prefill(p4q_dtype dt, int B, int L, int H, int D, const void *
                     B, H, L, (long long)ld);
     return hip_status(p4q::launch_attention(dt, B, L, H, q, k, v, ld, out, ld_out, causal, stream),
                       "p4q_attention_prefill");
+}
+
+// ---- serving: the paged cache and its attention ---------------------------------
+// Limits that the calls share.  Returns P4Q_OK or the failing status (message
+// recorded).
+static int check_heads(const char *who, p4q_dtype dt, int T, int B, int Hq, int Hk, int D) {
+    if (!valid_dtype(dt)) return fail(P4Q_ERR_UNSUPPORTED, "%s: dtype %d", who, (int)dt);
+    if (T <= 0 || B <= 0 || Hq <= 0 || Hk <= 0 || D <= 0 || Hq % Hk != 0)
+        return fail(P4Q_ERR_INVALID_ARG, "%s: T=%d B=%d Hq=%d Hk=%d D=%d (positive, Hq a multiple of Hk)", who, T, B,
+                    Hq, Hk, D);
+    if (D != 64 && D != 128) return fail(P4Q_ERR_UNSUPPORTED, "%s: head dimension %d (64 or 128)", who, D);
+    if (T > (1 << 24) || B > 65535 || Hq > 1024 || (int64_t)T * (Hq / Hk) >= (1LL << 31))
+        return fail(P4Q_ERR_UNSUPPORTED, "%s: T=%d B=%d Hq=%d Hk=%d too large", who, T, B, Hq, Hk);
+    return P4Q_OK;
+}
+
+static int check_stride(const char *who, const char *name, int64_t ld, int heads, int D) {
+    if (ld < (int64_t)heads * D || ld % 8 != 0)
+        return fail(P4Q_ERR_INVALID_ARG, "%s: row stride %lld of %s (need >= %lld, multiple of 8)", who, (long long)ld,
+                    name, (long long)heads * D);
+    if (ld >= (1 << 24)) return fail(P4Q_ERR_UNSUPPORTED, "%s: row stride %lld of %s >= 2^24", who, (long long)ld, name);
+    return P4Q_OK;
+}
+
+static int check_cache(const char *who, const void *k_cache, const void *v_cache, int num_pages, int page_size,
+                       const int32_t *table, int max_pages) {
+    if (!k_cache || !v_cache || !table) return fail(P4Q_ERR_INVALID_ARG, "%s: null pointer", who);
+    if (!aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(table, 4))
+        return fail(P4Q_ERR_INVALID_ARG, "%s: misaligned pointer", who);
+    if (num_pages <= 0 || max_pages <= 0)
+        return fail(P4Q_ERR_INVALID_ARG, "%s: num_pages=%d max_pages=%d", who, num_pages, max_pages);
+    if (p4q::page_shift(page_size) < 0)
+        return fail(P4Q_ERR_UNSUPPORTED, "%s: page size %d (a power of two from 16 to 4096)", who, page_size);
+    if ((int64_t)max_pages * page_size >= (1LL << 30))
+        return fail(P4Q_ERR_UNSUPPORTED, "%s: max_pages=%d of %d rows: 2^30 keys or more", who, max_pages, page_size);
+    return P4Q_OK;
+}
+
+int p4q_rope_append(p4q_dtype dt, int T, int B, int Hq, int Hk, int D, const void *q, int64_t ldq, const void *k,
+                    int64_t ldk, const void *v, int64_t ldv, const int32_t *cu_seqlens, const int32_t *cache_lens,
+                    const int32_t *positions, float rope_base, void *q_out, int64_t ldq_out, void *k_out,
+                    int64_t ldk_out, void *k_cache, void *v_cache, int num_pages, int page_size,
+                    const int32_t *block_table, int max_pages, hipStream_t stream) {
+    const char *who = "p4q_rope_append";
+    if (const int st = check_heads(who, dt, T, B, Hq, Hk, D)) return st;
+    if (!q || !k || !v || !q_out || !cu_seqlens) return fail(P4Q_ERR_INVALID_ARG, "%s: null pointer", who);
+    if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(q_out, 16) || !aligned(k_out, 16) ||
+        !aligned(cu_seqlens, 4) || !aligned(cache_lens, 4) || !aligned(positions, 4))
+        return fail(P4Q_ERR_INVALID_ARG, "%s: misaligned pointer", who);
+    if (const int st = check_stride(who, "q", ldq, Hq, D)) return st;
+    if (const int st = check_stride(who, "k", ldk, Hk, D)) return st;
+    if (const int st = check_stride(who, "v", ldv, Hk, D)) return st;
+    if (const int st = check_stride(who, "q_out", ldq_out, Hq, D)) return st;
+    if (k_out)
+        if (const int st = check_stride(who, "k_out", ldk_out, Hk, D)) return st;
+    if ((q_out == q && ldq_out != ldq) || (k_out == k && ldk_out != ldk))
+        return fail(P4Q_ERR_INVALID_ARG, "%s: an output in place needs its input's row stride", who);
+    if (!(rope_base > 1.0f) || !(rope_base < __builtin_huge_valf()))
+        return fail(P4Q_ERR_INVALID_ARG, "%s: rope_base=%g", who, (double)rope_base);
+    if (const int st = check_cache(who, k_cache, v_cache, num_pages, page_size, block_table, max_pages)) return st;
+    p4q::RopeAppend a{};
+    a.T = T, a.B = B, a.Hq = Hq, a.Hk = Hk;
+    a.q = static_cast<const uint16_t *>(q), a.k = static_cast<const uint16_t *>(k), a.v = static_cast<const uint16_t *>(v);
+    a.ldq = ldq, a.ldk = ldk, a.ldv = ldv;
+    a.cu = cu_seqlens, a.cache_lens = cache_lens, a.positions = positions;
+    a.q_out = static_cast<uint16_t *>(q_out), a.k_out = static_cast<uint16_t *>(k_out);
+    a.ldqo = ldq_out, a.ldko = ldk_out;
+    a.k_cache = static_cast<uint16_t *>(k_cache), a.v_cache = static_cast<uint16_t *>(v_cache);
+    a.num_pages = num_pages, a.shift = p4q::page_shift(page_size), a.max_pages = max_pages, a.table = block_table;
+    return hip_status(p4q::launch_rope_append(dt, D, a, rope_base, stream), who);
+}
+
+size_t p4q_attention_prompt_workspace_bytes(int T, int B, int Hq, int Hk, int D, int64_t most_keys) {
+    if (check_heads("", P4Q_FP16, T, B, Hq, Hk, D) != P4Q_OK || most_keys < 0 || most_keys >= (1LL << 31)) return 0;
+    return p4q::prompt_attention_workspace_bytes(T, B, Hq, Hk, D, most_keys);
+}
+
+int p4q_attention_packed(p4q_dtype dt, int T, int Tk, int B, int Hq, int Hk, int D, const void *q, int64_t ldq,
+                         const void *k, int64_t ldk, const void *v, int64_t ldv, const int32_t *cu_seqlens,
+                         const int32_t *cu_seqlens_k, void *out, int64_t ld_out, int causal, void *ws,
+                         size_t ws_bytes, hipStream_t stream) {
+    const char *who = "p4q_attention_packed";
+    if (const int st = check_heads(who, dt, T, B, Hq, Hk, D)) return st;
+    if (Tk < 0) return fail(P4Q_ERR_INVALID_ARG, "%s: Tk=%d", who, Tk);
+    if (Tk > (1 << 24)) return fail(P4Q_ERR_UNSUPPORTED, "%s: Tk=%d > 2^24", who, Tk);
+    if (causal != 0 && causal != 1) return fail(P4Q_ERR_INVALID_ARG, "%s: causal=%d", who, causal);
+    if (!q || !out || !cu_seqlens || (Tk > 0 && (!k || !v))) return fail(P4Q_ERR_INVALID_ARG, "%s: null pointer", who);
+    if (!cu_seqlens_k && Tk != T)
+        return fail(P4Q_ERR_INVALID_ARG, "%s: %d key rows for %d tokens need cu_seqlens_k", who, Tk, T);
+    if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(out, 16) || !aligned(cu_seqlens, 4) ||
+        !aligned(cu_seqlens_k, 4))
+        return fail(P4Q_ERR_INVALID_ARG, "%s: misaligned pointer", who);
+    if (const int st = check_stride(who, "q", ldq, Hq, D)) return st;
+    if (const int st = check_stride(who, "k", ldk, Hk, D)) return st;
+    if (const int st = check_stride(who, "v", ldv, Hk, D)) return st;
+    if (const int st = check_stride(who, "out", ld_out, Hq, D)) return st;
+    p4q::PromptAttention a{};
+    a.T = T, a.Tk = Tk, a.B = B, a.Hq = Hq, a.Hk = Hk;
+    a.q = static_cast<const uint16_t *>(q), a.k = static_cast<const uint16_t *>(k), a.v = static_cast<const uint16_t *>(v);
+    a.ldq = ldq, a.ldk = (int)ldk, a.ldv = (int)ldv, a.ldo = ld_out;
+    a.cu_q = cu_seqlens, a.cu_k = cu_seqlens_k ? cu_seqlens_k : cu_seqlens;
+    a.out = static_cast<uint16_t *>(out);
+    return hip_status(p4q::launch_prompt_attention(dt, D, a, causal, Tk, aligned(ws, 16) ? ws : nullptr,
+                                                   ws && aligned(ws, 16) ? ws_bytes : 0, stream), who);
+}
+
+int p4q_attention_prefill_paged(p4q_dtype dt, int T, int B, int Hq, int Hk, int D, const void *q, int64_t ldq,
+                                const void *k_cache, const void *v_cache, int num_pages, int page_size,
+                                const int32_t *block_table, int max_pages, const int32_t *cu_seqlens,
+                                const int32_t *seq_lens, void *out, int64_t ld_out, int causal, void *ws,
+                                size_t ws_bytes, hipStream_t stream) {
+    const char *who = "p4q_attention_prefill_paged";
+    if (const int st = check_heads(who, dt, T, B, Hq, Hk, D)) return st;
+    if (causal != 0 && causal != 1) return fail(P4Q_ERR_INVALID_ARG, "%s: causal=%d", who, causal);
+    if (!q || !out || !cu_seqlens || !seq_lens) return fail(P4Q_ERR_INVALID_ARG, "%s: null pointer", who);
+    if (!aligned(q, 16) || !aligned(out, 16) || !aligned(cu_seqlens, 4) || !aligned(seq_lens, 4))
+        return fail(P4Q_ERR_INVALID_ARG, "%s: misaligned pointer", who);
+    if (const int st = check_stride(who, "q", ldq, Hq, D)) return st;
+    if (const int st = check_stride(who, "out", ld_out, Hq, D)) return st;
+    if (const int st = check_cache(who, k_cache, v_cache, num_pages, page_size, block_table, max_pages)) return st;
+    p4q::PromptAttention a{};
+    a.T = T, a.B = B, a.Hq = Hq, a.Hk = Hk;
+    a.q = static_cast<const uint16_t *>(q), a.k = static_cast<const uint16_t *>(k_cache);
+    a.v = static_cast<const uint16_t *>(v_cache);
+    a.ldq = ldq, a.ldo = ld_out, a.cu_q = cu_seqlens, a.lens = seq_lens, a.table = block_table;
+    a.num_pages = num_pages, a.shift = p4q::page_shift(page_size), a.max_pages = max_pages;
+    a.out = static_cast<uint16_t *>(out);
+    return hip_status(p4q::launch_prompt_attention(dt, D, a, causal, (int64_t)max_pages * page_size,
+                                                   aligned(ws, 16) ? ws : nullptr,
+                                                   ws && aligned(ws, 16) ? ws_bytes : 0, stream), who);
+}
+
+size_t p4q_attention_decode_workspace_bytes(int B, int Hq, int Hk, int D, int max_len) {
+    if (check_heads("", P4Q_FP16, B, B, Hq, Hk, D) != P4Q_OK || max_len <= 0 || max_len >= (1 << 30)) return 0;
+    return p4q::decode_attention_workspace_bytes(B, Hq, Hk, D, max_len);
+}
+
+int p4q_attention_decode(p4q_dtype dt, int B, int Hq, int Hk, int D, const void *q, int64_t ldq, const void *k_cache,
+                         const void *v_cache, int num_pages, int page_size, const int32_t *block_table, int max_pages,
+                         const int32_t *seq_lens, int max_len, void *out, int64_t ld_out, void *ws, size_t ws_bytes,
+                         hipStream_t stream) {
+    const char *who = "p4q_attention_decode";
+    if (const int st = check_heads(who, dt, B, B, Hq, Hk, D)) return st;
+    if (!q || !out || !seq_lens) return fail(P4Q_ERR_INVALID_ARG, "%s: null pointer", who);
+    if (!aligned(q, 16) || !aligned(out, 16) || !aligned(seq_lens, 4))
+        return fail(P4Q_ERR_INVALID_ARG, "%s: misaligned pointer", who);
+    if (const int st = check_stride(who, "q", ldq, Hq, D)) return st;
+    if (const int st = check_stride(who, "out", ld_out, Hq, D)) return st;
+    if (const int st = check_cache(who, k_cache, v_cache, num_pages, page_size, block_table, max_pages)) return st;
+    if (max_len < 1 || max_len > (int64_t)max_pages * page_size)
+        return fail(P4Q_ERR_INVALID_ARG, "%s: max_len=%d outside [1, %lld]", who, max_len,
+                    (long long)max_pages * page_size);
+    const size_t need = p4q::decode_attention_workspace_bytes(B, Hq, Hk, D, max_len);
+    if (need > 0 && (!ws || ws_bytes < need))
+        return fail(P4Q_ERR_WORKSPACE, "%s: workspace %zu < %zu bytes", who, ws_bytes, need);
+    if (need > 0 && !aligned(ws, 16)) return fail(P4Q_ERR_INVALID_ARG, "%s: workspace not 16-byte aligned", who);
+    p4q::DecodeAttention a{};
+    a.B = B, a.Hq = Hq, a.Hk = Hk, a.max_len = max_len;
+    a.q = static_cast<const uint16_t *>(q), a.k = static_cast<const uint16_t *>(k_cache);
+    a.v = static_cast<const uint16_t *>(v_cache);
+    a.ldq = ldq, a.ldo = ld_out, a.lens = seq_lens, a.table = block_table;
+    a.num_pages = num_pages, a.shift = p4q::page_shift(page_size), a.max_pages = max_pages;
+    a.out = static_cast<uint16_t *>(out);
+    return hip_status(p4q::launch_decode_attention(dt, D, a, ws, stream), who);
 }
 
 static int calib_block_shape_error(int M, int d, int f, int H) {

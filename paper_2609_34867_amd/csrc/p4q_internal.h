@@ -66,6 +66,60 @@ hipError_t launch_attention(p4q_dtype dt, int B, int L, int H, const void *q, co
                             const void *v, int64_t ld, void *o, int64_t ldo, int causal,
                             hipStream_t stream);
 
+// ---- serving: the paged key-value cache and the attention that reads it --------
+// (kv_cache.h has the layout; `shift` is log2 of the page size.)  Fields behind
+// `set by the launcher` are the kernels' own.
+struct RopeAppend {
+    int T, B, Hq, Hk;
+    const uint16_t *q, *k, *v;
+    int64_t ldq, ldk, ldv;
+    const int32_t *cu, *cache_lens, *positions;      // the last two may be null
+    uint16_t *q_out, *k_out;                         // k_out may be null
+    int64_t ldqo, ldko;
+    uint16_t *k_cache, *v_cache;
+    int num_pages, shift, max_pages;
+    const int32_t *table;
+    // set by the launcher
+    int parts;                                       // wavefronts per token
+    double log2_ratio;                               // log2(theta_1 / theta_0)
+};
+hipError_t launch_rope_append(p4q_dtype dt, int D, RopeAppend a, float rope_base, hipStream_t stream);
+
+struct PromptAttention {
+    int T, Tk, B, Hq, Hk;
+    const uint16_t *q, *k, *v;                       // k and v: packed rows, or the caches
+    int64_t ldq, ldo;
+    int ldk, ldv;                                    // packed
+    const int32_t *cu_q, *cu_k;                      // cu_k: packed
+    const int32_t *lens, *table;                     // the cache's (table null: packed)
+    int num_pages, shift, max_pages;
+    uint16_t *out;
+    // set by the launcher
+    int G, tiles, splits;
+    float c2;
+    float *part;
+};
+// most_keys: a bound of the keys of a sequence
+size_t prompt_attention_workspace_bytes(int T, int B, int Hq, int Hk, int D, int64_t most_keys);
+hipError_t launch_prompt_attention(p4q_dtype dt, int D, PromptAttention a, int causal, int64_t most_keys, void *ws,
+                                   size_t ws_bytes, hipStream_t stream);
+
+struct DecodeAttention {
+    int B, Hq, Hk, max_len;
+    const uint16_t *q, *k, *v;                       // k and v: the caches
+    int64_t ldq, ldo;
+    const int32_t *lens, *table;
+    int num_pages, shift, max_pages;
+    uint16_t *out;
+    // set by the launcher
+    int G, chunk;
+    float c2;
+    uint32_t *arrivals;
+    float *part;
+};
+size_t decode_attention_workspace_bytes(int B, int Hq, int Hk, int D, int max_len);
+hipError_t launch_decode_attention(p4q_dtype dt, int D, DecodeAttention a, void *ws, hipStream_t stream);
+
 // ---- selector ---------------------------------------------------------------
 struct SelectWorkspace {
     int32_t *stats;      // [B][N][J+1]: D_0..D_{J-1}, Nv   (documented)
