@@ -27,11 +27,13 @@ def _dtype_code(t: torch.dtype) -> int:
 
 
 def _ptr(t: Optional[torch.Tensor]):
-    return None if t is None else ctypes.c_void_p(t.data_ptr())
+    return None if t is None else t.data_ptr()
 
 
 def _stream(dev: torch.device):
-    return ctypes.c_void_p(torch.cuda.current_stream(dev).cuda_stream)
+    """The handle of dev's current stream (torch.cuda.current_stream(dev).cuda_stream
+    without the stream object: 0.1 instead of 1.9 us of every call)."""
+    return torch._C._cuda_getCurrentRawStream(dev.index)
 
 
 def _need_gpu(*ts):
@@ -294,19 +296,24 @@ def attention_prefill(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, B: int,
 
 
 # --------------------------------------------------------------------------- serving
-def _rows_of(t: torch.Tensor, name: str, rows: Optional[int], cols: int, dtype) -> None:
-    """A 2-D operand [rows, >= cols] whose rows may be columns of a wider buffer."""
-    if t.dim() != 2 or t.shape[1] < cols or (rows is not None and t.shape[0] != rows):
-        raise ValueError(f"{name} must have shape ({'rows' if rows is None else rows}, >= {cols}), got {tuple(t.shape)}")
-    if t.stride(1) != 1:
+def _rows_of(t: torch.Tensor, name: str, rows: int, cols: int, dtype) -> int:
+    """Checks a 2-D operand [rows, >= cols], whose rows may be columns of a wider
+    buffer, and returns its row stride (a single row may have any: its width)."""
+    shape = t.shape
+    if len(shape) != 2 or shape[0] != rows or shape[1] < cols:
+        raise ValueError(f"{name} must have shape ({rows}, >= {cols}), got {tuple(shape)}")
+    ld, unit = t.stride()
+    if unit != 1:
         raise ValueError(f"{name} must have unit column stride")
     if t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    return ld if rows > 1 else max(cols, ld) // 8 * 8
 
 
-def _ld(t: torch.Tensor, cols: int) -> int:
-    """Row stride of a 2-D operand (one row may have any: its own width then)."""
-    return t.stride(0) if t.shape[0] > 1 else max(cols, t.stride(0)) // 8 * 8
+def _elsewhere(dev: torch.device) -> bool:
+    """Whether a call on dev's tensors has to make dev the current device first
+    (launches and the sizes of workspaces go by the current one)."""
+    return dev.index != torch.cuda.current_device()
 
 
 def _ints(t: Optional[torch.Tensor], name: str, n: int) -> None:
@@ -318,7 +325,8 @@ def _cache_shape(k_cache: torch.Tensor, v_cache: torch.Tensor, block_table: torc
     """(pages, Hk, page size, D, B, table width) of a paged cache and its table."""
     if q.dtype not in _F16:
         raise ValueError(f"q must be fp16 or bf16, got {q.dtype}")
-    if k_cache.dim() != 4 or k_cache.shape != v_cache.shape:
+    shape = k_cache.shape
+    if len(shape) != 4 or shape != v_cache.shape:
         raise ValueError("k_cache and v_cache must share a shape [pages, Hk, page size, D]")
     if k_cache.dtype != q.dtype or v_cache.dtype != q.dtype:
         raise ValueError("the caches must have q's dtype")
@@ -326,7 +334,7 @@ def _cache_shape(k_cache: torch.Tensor, v_cache: torch.Tensor, block_table: torc
         raise ValueError("k_cache and v_cache must be contiguous")
     if block_table.dim() != 2 or block_table.dtype != torch.int32 or not block_table.is_contiguous():
         raise ValueError("block_table must be a contiguous int32 [B, max_pages] tensor")
-    pages, Hk, page, D = k_cache.shape
+    pages, Hk, page, D = shape
     if Hk < 1 or Hq < 1 or Hq % Hk:
         raise ValueError(f"Hq = {Hq} is not a multiple of the cache's {Hk} key heads")
     return pages, Hk, page, D, block_table.shape[0], block_table.shape[1]
@@ -348,26 +356,30 @@ def rope_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqlens: t
     k_out.  q_out may be q, k_out may be k.  Rows behind the last sequence are
     left as they were."""
     pages, Hk, page, D, B, width = _cache_shape(k_cache, v_cache, block_table, q, Hq)
-    T = q.shape[0]
-    _rows_of(q, "q", None, Hq * D, q.dtype)
-    _rows_of(k, "k", T, Hk * D, q.dtype)
-    _rows_of(v, "v", T, Hk * D, q.dtype)
+    T, dt = q.shape[0], q.dtype
+    ldq = _rows_of(q, "q", T, Hq * D, dt)
+    ldk = _rows_of(k, "k", T, Hk * D, dt)
+    ldv = _rows_of(v, "v", T, Hk * D, dt)
     _ints(cu_seqlens, "cu_seqlens", B + 1)
     _ints(cache_lens, "cache_lens", B)
     _ints(positions, "positions", T)
+    ldqo = ldko = 0
     if q_out is not None:
-        _rows_of(q_out, "q_out", T, Hq * D, q.dtype)
+        ldqo = _rows_of(q_out, "q_out", T, Hq * D, dt)
     if k_out is not None:
-        _rows_of(k_out, "k_out", T, Hk * D, q.dtype)
+        ldko = _rows_of(k_out, "k_out", T, Hk * D, dt)
     _need_gpu(q, k, v, cu_seqlens, block_table, k_cache, v_cache, cache_lens, positions, q_out, k_out)
-    with torch.cuda.device(q.device):
-        if q_out is None:
-            q_out = torch.empty((T, Hq * D), dtype=q.dtype, device=q.device)
-        check(lib().p4q_rope_append(
-            _dtype_code(q.dtype), T, B, Hq, Hk, D, _ptr(q), _ld(q, Hq * D), _ptr(k), _ld(k, Hk * D), _ptr(v),
-            _ld(v, Hk * D), _ptr(cu_seqlens), _ptr(cache_lens), _ptr(positions), rope_base, _ptr(q_out),
-            _ld(q_out, Hq * D), _ptr(k_out), 0 if k_out is None else _ld(k_out, Hk * D), _ptr(k_cache),
-            _ptr(v_cache), pages, page, _ptr(block_table), width, _stream(q.device)))
+    dev = q.device
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return rope_append(q, k, v, cu_seqlens, block_table, k_cache, v_cache, Hq, cache_lens, positions,
+                               rope_base, q_out, k_out)
+    if q_out is None:
+        q_out, ldqo = torch.empty((T, Hq * D), dtype=dt, device=dev), Hq * D
+    check(lib().p4q_rope_append(
+        _dtype_code(dt), T, B, Hq, Hk, D, _ptr(q), ldq, _ptr(k), ldk, _ptr(v), ldv, _ptr(cu_seqlens),
+        _ptr(cache_lens), _ptr(positions), rope_base, _ptr(q_out), ldqo, _ptr(k_out), ldko, _ptr(k_cache),
+        _ptr(v_cache), pages, page, _ptr(block_table), width, _stream(dev)))
     return q_out, k_out
 
 
@@ -384,8 +396,9 @@ def attention_prompt_workspace(T: int, B: int, Hq: int, Hk: int, D: int, most_ke
 def _own_prompt_workspace(T, B, Hq, Hk, D, most_keys, device) -> Optional[torch.Tensor]:
     """Workspace of one call that was given none; a device without room for it
     runs the call unsplit."""
+    n = lib().p4q_attention_prompt_workspace_bytes(T, B, Hq, Hk, D, most_keys)
     try:
-        return attention_prompt_workspace(T, B, Hq, Hk, D, most_keys, device)
+        return torch.empty(n, dtype=torch.uint8, device=device) if n else None
     except torch.OutOfMemoryError:
         return None
 
@@ -401,10 +414,10 @@ def attention_packed(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqle
     rows behind the last sequence are left as they were."""
     if q.dtype not in _F16:
         raise ValueError(f"q must be fp16 or bf16, got {q.dtype}")
-    T, Tk = q.shape[0], k.shape[0]
-    _rows_of(q, "q", None, Hq * D, q.dtype)
-    _rows_of(k, "k", None, Hk * D, q.dtype)
-    _rows_of(v, "v", Tk, Hk * D, q.dtype)
+    T, Tk, dt = q.shape[0], k.shape[0], q.dtype
+    ldq = _rows_of(q, "q", T, Hq * D, dt)
+    ldk = _rows_of(k, "k", Tk, Hk * D, dt)
+    ldv = _rows_of(v, "v", Tk, Hk * D, dt)
     if cu_seqlens.dim() != 1 or cu_seqlens.shape[0] < 2:
         raise ValueError(f"cu_seqlens must have shape (B + 1,), got {tuple(cu_seqlens.shape)}")
     B = cu_seqlens.shape[0] - 1
@@ -412,19 +425,21 @@ def attention_packed(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqle
     _ints(cu_seqlens_k, "cu_seqlens_k", B + 1)
     if cu_seqlens_k is None and Tk != T:
         raise ValueError(f"k has {Tk} rows and q {T}: cu_seqlens_k is needed")
-    if out is not None:
-        _rows_of(out, "out", T, Hq * D, q.dtype)
+    ldo = Hq * D if out is None else _rows_of(out, "out", T, Hq * D, dt)
     _check(workspace, "workspace", None, torch.uint8)
     _need_gpu(q, k, v, cu_seqlens, cu_seqlens_k, out, workspace)
-    with torch.cuda.device(q.device):
-        if out is None:
-            out = torch.empty((T, Hq * D), dtype=q.dtype, device=q.device)
-        if workspace is None:
-            workspace = _own_prompt_workspace(T, B, Hq, Hk, D, Tk, q.device)
-        check(lib().p4q_attention_packed(
-            _dtype_code(q.dtype), T, Tk, B, Hq, Hk, D, _ptr(q), _ld(q, Hq * D), _ptr(k), _ld(k, Hk * D), _ptr(v),
-            _ld(v, Hk * D), _ptr(cu_seqlens), _ptr(cu_seqlens_k), _ptr(out), _ld(out, Hq * D), int(causal),
-            _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream(q.device)))
+    dev = q.device
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return attention_packed(q, k, v, cu_seqlens, Hq, Hk, D, causal, cu_seqlens_k, out, workspace)
+    if out is None:
+        out = torch.empty((T, Hq * D), dtype=dt, device=dev)
+    if workspace is None:
+        workspace = _own_prompt_workspace(T, B, Hq, Hk, D, Tk, dev)
+    check(lib().p4q_attention_packed(
+        _dtype_code(dt), T, Tk, B, Hq, Hk, D, _ptr(q), ldq, _ptr(k), ldk, _ptr(v), ldv, _ptr(cu_seqlens),
+        _ptr(cu_seqlens_k), _ptr(out), ldo, int(causal), _ptr(workspace),
+        0 if workspace is None else workspace.numel(), _stream(dev)))
     return out
 
 
@@ -438,23 +453,26 @@ def attention_prefill_paged(q: torch.Tensor, k_cache: torch.Tensor, v_cache: tor
     of each sequence, its tokens of this call included); the rest as
     attention_packed() and rope_append()."""
     pages, Hk, page, D, B, width = _cache_shape(k_cache, v_cache, block_table, q, Hq)
-    T = q.shape[0]
-    _rows_of(q, "q", None, Hq * D, q.dtype)
+    T, dt = q.shape[0], q.dtype
+    ldq = _rows_of(q, "q", T, Hq * D, dt)
     _ints(cu_seqlens, "cu_seqlens", B + 1)
     _ints(seq_lens, "seq_lens", B)
-    if out is not None:
-        _rows_of(out, "out", T, Hq * D, q.dtype)
+    ldo = Hq * D if out is None else _rows_of(out, "out", T, Hq * D, dt)
     _check(workspace, "workspace", None, torch.uint8)
     _need_gpu(q, k_cache, v_cache, cu_seqlens, block_table, seq_lens, out, workspace)
-    with torch.cuda.device(q.device):
-        if out is None:
-            out = torch.empty((T, Hq * D), dtype=q.dtype, device=q.device)
-        if workspace is None:
-            workspace = _own_prompt_workspace(T, B, Hq, Hk, D, width * page, q.device)
-        check(lib().p4q_attention_prefill_paged(
-            _dtype_code(q.dtype), T, B, Hq, Hk, D, _ptr(q), _ld(q, Hq * D), _ptr(k_cache), _ptr(v_cache), pages,
-            page, _ptr(block_table), width, _ptr(cu_seqlens), _ptr(seq_lens), _ptr(out), _ld(out, Hq * D),
-            int(causal), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream(q.device)))
+    dev = q.device
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return attention_prefill_paged(q, k_cache, v_cache, cu_seqlens, block_table, seq_lens, Hq, causal, out,
+                                           workspace)
+    if out is None:
+        out = torch.empty((T, Hq * D), dtype=dt, device=dev)
+    if workspace is None:
+        workspace = _own_prompt_workspace(T, B, Hq, Hk, D, width * page, dev)
+    check(lib().p4q_attention_prefill_paged(
+        _dtype_code(dt), T, B, Hq, Hk, D, _ptr(q), ldq, _ptr(k_cache), _ptr(v_cache), pages, page,
+        _ptr(block_table), width, _ptr(cu_seqlens), _ptr(seq_lens), _ptr(out), ldo, int(causal), _ptr(workspace),
+        0 if workspace is None else workspace.numel(), _stream(dev)))
     return out
 
 
@@ -480,23 +498,26 @@ def attention_decode(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
     needs one; a given one must come from attention_decode_workspace() and serve one
     call at a time.  Returns out [B, Hq*D]."""
     pages, Hk, page, D, B, width = _cache_shape(k_cache, v_cache, block_table, q, Hq)
-    _rows_of(q, "q", B, Hq * D, q.dtype)
+    dt = q.dtype
+    ldq = _rows_of(q, "q", B, Hq * D, dt)
     _ints(seq_lens, "seq_lens", B)
-    if out is not None:
-        _rows_of(out, "out", B, Hq * D, q.dtype)
+    ldo = Hq * D if out is None else _rows_of(out, "out", B, Hq * D, dt)
     _check(workspace, "workspace", None, torch.uint8)
     _need_gpu(q, k_cache, v_cache, block_table, seq_lens, out, workspace)
+    dev = q.device
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return attention_decode(q, k_cache, v_cache, block_table, seq_lens, Hq, max_len, out, workspace)
     if max_len is None:
         max_len = width * page
-    with torch.cuda.device(q.device):
-        if out is None:
-            out = torch.empty((B, Hq * D), dtype=q.dtype, device=q.device)
-        if workspace is None:
-            workspace = attention_decode_workspace(B, Hq, Hk, D, max_len, q.device)
-        check(lib().p4q_attention_decode(
-            _dtype_code(q.dtype), B, Hq, Hk, D, _ptr(q), _ld(q, Hq * D), _ptr(k_cache), _ptr(v_cache), pages, page,
-            _ptr(block_table), width, _ptr(seq_lens), max_len, _ptr(out), _ld(out, Hq * D), _ptr(workspace),
-            0 if workspace is None else workspace.numel(), _stream(q.device)))
+    if out is None:
+        out = torch.empty((B, Hq * D), dtype=dt, device=dev)
+    if workspace is None:
+        workspace = attention_decode_workspace(B, Hq, Hk, D, max_len, dev)
+    check(lib().p4q_attention_decode(
+        _dtype_code(dt), B, Hq, Hk, D, _ptr(q), ldq, _ptr(k_cache), _ptr(v_cache), pages, page, _ptr(block_table),
+        width, _ptr(seq_lens), max_len, _ptr(out), ldo, _ptr(workspace),
+        0 if workspace is None else workspace.numel(), _stream(dev)))
     return out
 
 
