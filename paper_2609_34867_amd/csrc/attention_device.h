@@ -13,6 +13,7 @@ typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 typedef _Float16 v2h __attribute__((ext_vector_type(2)));
 typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
 typedef float v2f __attribute__((ext_vector_type(2)));
+typedef int v2i __attribute__((ext_vector_type(2)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 typedef short v4s __attribute__((ext_vector_type(4)));
@@ -71,6 +72,14 @@ __device__ __forceinline__ float xmax16(float x) {
 __device__ __forceinline__ float xsum16(float x) {
     const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return __uint_as_float(p[0]) + __uint_as_float(p[1]);
+}
+
+// p[i], i the same in all lanes, by a scalar load: for lists that nobody writes
+// while the kernel runs (lengths, block tables).  A vector load would queue in
+// order with the loads of keys and values, and so would the wait for it.
+__device__ __forceinline__ int32_t uniform_load(const int32_t *p, int64_t i) {
+    typedef const __attribute__((address_space(4))) int32_t *constant_t;
+    return reinterpret_cast<constant_t>(reinterpret_cast<uint64_t>(p))[i];
 }
 
 }  // namespace

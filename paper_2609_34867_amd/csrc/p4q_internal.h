@@ -112,7 +112,7 @@ struct DecodeAttention {
     int num_pages, shift, max_pages;
     uint16_t *out;
     // set by the launcher
-    int G, chunk;
+    int G;
     float c2;
     uint32_t *arrivals;
     float *part;
