@@ -52,4 +52,20 @@ constexpr Span packed_span(int begin, int end, int total) {
     return Span{f, l};
 }
 
+// n / G for n < 2^31 as (2 n m) >> (32 + s), with s = ceil(log2 G) and
+// m = floor(2^(31 + s) / G) + 1 <= 2^32 - 1:  m G = 2^(31 + s) + e with 0 < e <= G <= 2^s,
+// so n m / 2^(31 + s) exceeds n / G by less than n / 2^31 / G < 1 / G.
+struct Magic {
+    uint32_t m;
+    int shift;
+};
+constexpr Magic magic_of(int G) {
+    int s = 0;
+    while ((1 << s) < G) ++s;
+    return Magic{(uint32_t)(((uint64_t)1 << (31 + s)) / (uint32_t)G + 1), s};
+}
+constexpr int magic_div(int n, uint32_t m, int shift) {
+    return (int)((uint32_t)(((uint64_t)(2u * (uint32_t)n) * m) >> 32) >> shift);
+}
+
 }  // namespace p4q

@@ -96,7 +96,9 @@ struct PromptAttention {
     uint16_t *out;
     // set by the launcher
     int G, tiles, splits;
-    float c2;
+    uint32_t g_magic;                                // division by G (kv_cache.h)
+    int g_shift;
+    float c2, split_gain;
     float *part;
 };
 // most_keys: a bound of the keys of a sequence

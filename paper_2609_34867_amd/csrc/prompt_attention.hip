@@ -47,7 +47,7 @@ constexpr int kQB = kNW * kQW;          // rows per work-group
 constexpr int kKT = 64;                 // keys per tile
 constexpr float kRescale = 8.0f;        // raise the running max past this margin (exp2 units)
 constexpr int kSplitTiles = 4;          // a split has at least this many tiles (if the row tile has)
-constexpr int kMaxSplits = 16;
+constexpr int kMaxSplits = 32;
 
 // LDS placement of 16-byte chunk c of row r (D/8 chunks).  K: the rows that a
 // fragment read takes together (16 of them, one chunk) fall in distinct banks; V:
@@ -74,54 +74,43 @@ struct RowTile {
 
 template <bool CAUSAL, bool PAGED>
 __device__ __forceinline__ RowTile find_tile(const PromptAttention &a, int x, int lane) {
+    auto by_g = [&](int r) __attribute__((always_inline)) { return magic_div(r, a.g_magic, a.g_shift); };
     RowTile t;
     t.b = -1;
     int before = 0;                     // row tiles of the sequences before this batch of 64
     for (int i = 0; i < a.B; i += 64) {
-        int n = 0;
-        if (i + lane < a.B) {
-            const Span s = packed_span(a.cu_q[i + lane], a.cu_q[i + lane + 1], a.T);
-            n = s.last - s.first;
-        }
+        // (lanes past the last sequence look at the last one's lists)
+        const int b = min(i + lane, a.B - 1);
+        const Span q = packed_span(a.cu_q[b], a.cu_q[b + 1], a.T);
+        const Span k = PAGED ? Span{0, key_count(a.lens[b])} : packed_span(a.cu_k[b], a.cu_k[b + 1], a.Tk);
+        const int n = i + lane < a.B ? q.last - q.first : 0;
         const int tiles = (int)(((uint32_t)n * (uint32_t)a.G + (uint32_t)(kQB - 1)) / (uint32_t)kQB);
         const int upto = before + (int)wave_inclusive_scan((uint32_t)tiles);
-        const uint64_t done = __ballot(upto <= x);
-        const int k = __popcll(done);   // sequences of the batch that end before tile x (they ascend)
-        if (k < 64 && i + k < a.B) {
-            const int b = i + k;
-            const Span s = packed_span(a.cu_q[b], a.cu_q[b + 1], a.T);
-            t.b = b;
-            t.first = s.first;
-            t.n = s.last - s.first;
+        const int at = __popcll(__ballot(upto <= x));   // sequences that end before tile x (they ascend)
+        if (at < 64) {
+            t.b = i + at;
+            t.first = __builtin_amdgcn_readlane(q.first, at);
+            t.n = __builtin_amdgcn_readlane(n, at);
+            t.kfirst = __builtin_amdgcn_readlane(k.first, at);
+            t.m = __builtin_amdgcn_readlane(k.last, at) - t.kfirst;
+            t.cap = PAGED ? min(t.m, a.max_pages << a.shift) : t.m;
             t.rows = t.n * a.G;
-            const int mine = (t.rows + kQB - 1) / kQB;
-            const int from = __builtin_amdgcn_readlane(upto, k) - mine;
-            const int q = x - from;
-            t.r0 = (CAUSAL ? mine - 1 - q : q) * kQB;          // longest (causal) first
+            const int mine = __builtin_amdgcn_readlane(tiles, at), j = x - (__builtin_amdgcn_readlane(upto, at) - mine);
+            t.r0 = (CAUSAL ? mine - 1 - j : j) * kQB;           // longest (causal) first
             break;
         }
         before = __builtin_amdgcn_readlane(upto, 63);
     }
     if (t.b < 0) return t;
-    if (PAGED) {
-        t.kfirst = 0;
-        t.m = key_count(a.lens[t.b]);
-        t.cap = min(t.m, a.max_pages << a.shift);
-    } else {
-        const Span s = packed_span(a.cu_k[t.b], a.cu_k[t.b + 1], a.Tk);
-        t.kfirst = s.first;
-        t.m = s.last - s.first;
-        t.cap = t.m;
-    }
     const int last = min(t.r0 + kQB, t.rows) - 1;
-    const int keys = CAUSAL ? min(t.cap, max(0, last / a.G + 1 + t.m - t.n)) : t.cap;
+    const int keys = CAUSAL ? min(t.cap, max(0, by_g(last) + 1 + t.m - t.n)) : t.cap;
     t.ntiles = (keys + kKT - 1) / kKT;
-    t.splits = max(1, min(a.splits, t.ntiles / kSplitTiles));
+    t.splits = max(1, min(min(a.splits, t.ntiles / kSplitTiles), (int)__builtin_sqrtf((float)t.ntiles * a.split_gain)));
     return t;
 }
 
 template <bool BF16, int D, bool CAUSAL, bool PAGED>
-__global__ __launch_bounds__(64 * kNW, 2) void k_prompt_attention(PromptAttention a) {
+__global__ __launch_bounds__(64 * kNW, D == 64 ? 3 : 2) void k_prompt_attention(PromptAttention a) {
     constexpr int kRow = 2 * D;             // bytes of a K or V row
     constexpr int kOperand = kKT * kRow;
     constexpr int kTile = 2 * kOperand;     // K, then V
@@ -149,14 +138,15 @@ __global__ __launch_bounds__(64 * kNW, 2) void k_prompt_attention(PromptAttentio
     const int shift_rows = t.m - t.n;                       // causal: token i sees keys up to i + m - n
 
     // this wavefront's rows, and this lane's
+    auto by_g = [&](int r) __attribute__((always_inline)) { return magic_div(r, a.g_magic, a.g_shift); };
     const int rw0 = t.r0 + kQW * wave;
     const int row = min(rw0 + c32, t.rows - 1);             // rows past the last take its query; not stored
-    const int tok = row / a.G, hq = hk * a.G + (row - tok * a.G);
+    const int tok = by_g(row), hq = hk * a.G + (row - tok * a.G);
     const int seen = CAUSAL ? min(t.m, tok + 1 + shift_rows) : t.m;     // keys that this row sees (or <= 0)
     // keys that some row, or every row, of the wavefront sees
     const int wlast = min(rw0 + kQW, t.rows) - 1;
-    const int most = rw0 >= t.rows ? 0 : CAUSAL ? max(0, min(t.cap, wlast / a.G + 1 + shift_rows)) : t.cap;
-    const int least = CAUSAL ? min(t.m, min(rw0, t.rows - 1) / a.G + 1 + shift_rows) : t.m;
+    const int most = rw0 >= t.rows ? 0 : CAUSAL ? max(0, min(t.cap, by_g(wlast) + 1 + shift_rows)) : t.cap;
+    const int least = CAUSAL ? min(t.m, by_g(min(rw0, t.rows - 1)) + 1 + shift_rows) : t.m;
 
     // DMA of a tile: instruction n of a wavefront fills rows 16 wave + kRpi n + lane / kChunks of
     // the operand; slot lane % kChunks takes the chunk that k_slot / v_slot place there (both are
@@ -174,7 +164,7 @@ __global__ __launch_bounds__(64 * kNW, 2) void k_prompt_attention(PromptAttentio
     // the page of this wavefront's rows of tile kt (PAGED; a tile past the last: any)
     auto page_of = [&](int kt) __attribute__((always_inline)) {
         if constexpr (!PAGED) return 0;
-        else return table[min((kt * kKT + 16 * wave) >> a.shift, a.max_pages - 1)];
+        else return uniform_load(table, min((kt * kKT + 16 * wave) >> a.shift, a.max_pages - 1));
     };
     // (no tile kt: empty descriptors, nothing is read)
     auto issue = [&](bool isv, int kt, int page) __attribute__((always_inline)) {
@@ -377,6 +367,7 @@ __global__ __launch_bounds__(64 * kNW, 2) void k_prompt_attention(PromptAttentio
         // unnormalized sums, maximum and sum of every row, for the joining launch
         float *part = a.part + (int64_t)(unit * a.splits + z) * kQB * (D + 2);
         float *dst = part + (int64_t)(kQW * wave + c32) * D + 4 * g;
+        if (rw0 + c32 >= t.rows) return;
 #pragma unroll
         for (int db = 0; db < kBlocks; ++db)
 #pragma unroll
@@ -410,7 +401,7 @@ __global__ __launch_bounds__(64 * kNW, 2) void k_prompt_attention(PromptAttentio
         const int r = kRpi * s + lane / kChunks, rr = rw0 + r;
         const uint4 w = *reinterpret_cast<const uint4 *>(stg + r * kRow + 16 * ((lane & (kChunks - 1)) ^ (r & (kChunks - 1))));
         if (rr < t.rows) {
-            const int i = rr / a.G, h = hk * a.G + (rr - i * a.G);
+            const int i = by_g(rr), h = hk * a.G + (rr - i * a.G);
             uint16_t *dst = a.out + (int64_t)(t.first + i) * a.ldo + (int64_t)h * D + 8 * (lane & (kChunks - 1));
             __builtin_nontemporal_store(__builtin_bit_cast(v4i, w), reinterpret_cast<v4i *>(dst));
         }
@@ -446,7 +437,7 @@ __global__ __launch_bounds__(256) void k_prompt_join(PromptAttention a) {
             o.z = o.z * f + x.z * e;
             o.w = o.w * f + x.w * e;
         }
-        const int i = row / a.G, h = hk * a.G + (row - i * a.G);
+        const int i = magic_div(row, a.g_magic, a.g_shift), h = hk * a.G + (row - i * a.G);
         const int seen = CAUSAL ? i + 1 + t.m - t.n : t.m;
         const float inv = 1.0f / l;
         uint2 w = make_uint2(pack2_scaled<BF16>(o.x, o.y, inv), pack2_scaled<BF16>(o.z, o.w, inv));
@@ -458,18 +449,23 @@ __global__ __launch_bounds__(256) void k_prompt_join(PromptAttention a) {
 // row tiles per key head, never fewer than the sequences have
 int64_t row_tiles(int T, int B, int G) { return (int64_t)T * G / kQB + B; }
 
+// What a split saves is the time of the tiles, about 1.3 us each; what it costs is the
+// join: 33 ns per row tile and split to write and read the sums.  The sum of both
+// is least at sqrt(tiles * gain) splits.
+float split_gain(int T, int Hq) { return 40.0f * kQB / ((float)T * (float)Hq); }
+
 // work-groups that share the keys of a row tile, at most
-int prompt_splits(int64_t units, int64_t most_keys) {
-    const int64_t want = 2 * (int64_t)device_cus();
-    const int64_t tiles = (most_keys + kKT - 1) / kKT;
-    return (int)std::max<int64_t>(1, std::min<int64_t>({want / units, tiles / kSplitTiles, (int64_t)kMaxSplits}));
+int prompt_splits(int T, int B, int Hq, int Hk, int64_t most_keys) {
+    const int64_t tiles = (most_keys + kKT - 1) / kKT, units = row_tiles(T, B, Hq / Hk) * Hk;
+    const int64_t best = (int64_t)__builtin_sqrtf((float)tiles * split_gain(T, Hq));
+    return (int)std::max<int64_t>(1, std::min<int64_t>({2 * device_cus() / units, tiles / kSplitTiles, best, (int64_t)kMaxSplits}));
 }
 
 }  // namespace
 
 size_t prompt_attention_workspace_bytes(int T, int B, int Hq, int Hk, int D, int64_t most_keys) {
     const int64_t units = row_tiles(T, B, Hq / Hk) * Hk;
-    const int splits = prompt_splits(units, most_keys);
+    const int splits = prompt_splits(T, B, Hq, Hk, most_keys);
     return splits > 1 ? (size_t)(units * splits * kQB * (D + 2)) * 4 : 0;
 }
 
@@ -477,8 +473,11 @@ hipError_t launch_prompt_attention(p4q_dtype dt, int D, PromptAttention a, int c
                                    size_t ws_bytes, hipStream_t stream) {
     a.c2 = 1.4426950408889634f / __builtin_sqrtf((float)D);                 // log2(e) / sqrt(D)
     a.G = a.Hq / a.Hk;
+    const Magic g = magic_of(a.G);
+    a.g_magic = g.m, a.g_shift = g.shift;
     const int64_t tiles = row_tiles(a.T, a.B, a.G), units = tiles * a.Hk;
-    a.splits = prompt_splits(units, most_keys);
+    a.splits = prompt_splits(a.T, a.B, a.Hq, a.Hk, most_keys);
+    a.split_gain = split_gain(a.T, a.Hq);
     if (ws_bytes < prompt_attention_workspace_bytes(a.T, a.B, a.Hq, a.Hk, D, most_keys)) a.splits = 1;
     a.part = static_cast<float *>(ws);
     if (units * a.splits > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
