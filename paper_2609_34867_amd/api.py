@@ -310,14 +310,21 @@ def _rows_of(t: torch.Tensor, name: str, rows: int, cols: int, dtype) -> int:
     return ld if rows > 1 else max(cols, ld) // 8 * 8
 
 
-def _elsewhere(dev: torch.device) -> bool:
-    """Whether a call on dev's tensors has to make dev the current device first
-    (launches and the sizes of workspaces go by the current one)."""
-    return dev.index != torch.cuda.current_device()
+def _elsewhere(q: torch.Tensor, *ts: Optional[torch.Tensor]) -> bool:
+    """Checks that all tensors live on one GPU, and returns whether that has to be
+    made the current device first (launches and the sizes of workspaces go by the
+    current one)."""
+    i = q.get_device()
+    for t in ts:
+        if t is not None and t.get_device() != i:
+            _need_gpu(q, *ts)
+    if i < 0:
+        _need_gpu(q)
+    return i != torch.cuda.current_device()
 
 
 def _ints(t: Optional[torch.Tensor], name: str, n: int) -> None:
-    if t is not None and (t.shape != (n,) or t.dtype != torch.int32 or not t.is_contiguous()):
+    if t is not None and (t.dtype is not torch.int32 or t.shape != (n,) or not t.is_contiguous()):
         raise ValueError(f"{name} must be a contiguous int32 tensor of shape ({n},), got {t.dtype} {tuple(t.shape)}")
 
 
@@ -368,9 +375,8 @@ def rope_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqlens: t
         ldqo = _rows_of(q_out, "q_out", T, Hq * D, dt)
     if k_out is not None:
         ldko = _rows_of(k_out, "k_out", T, Hk * D, dt)
-    _need_gpu(q, k, v, cu_seqlens, block_table, k_cache, v_cache, cache_lens, positions, q_out, k_out)
     dev = q.device
-    if _elsewhere(dev):
+    if _elsewhere(q, k, v, cu_seqlens, block_table, k_cache, v_cache, cache_lens, positions, q_out, k_out):
         with torch.cuda.device(dev):
             return rope_append(q, k, v, cu_seqlens, block_table, k_cache, v_cache, Hq, cache_lens, positions,
                                rope_base, q_out, k_out)
@@ -426,10 +432,10 @@ def attention_packed(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqle
     if cu_seqlens_k is None and Tk != T:
         raise ValueError(f"k has {Tk} rows and q {T}: cu_seqlens_k is needed")
     ldo = Hq * D if out is None else _rows_of(out, "out", T, Hq * D, dt)
-    _check(workspace, "workspace", None, torch.uint8)
-    _need_gpu(q, k, v, cu_seqlens, cu_seqlens_k, out, workspace)
+    if workspace is not None:
+        _check(workspace, "workspace", None, torch.uint8)
     dev = q.device
-    if _elsewhere(dev):
+    if _elsewhere(q, k, v, cu_seqlens, cu_seqlens_k, out, workspace):
         with torch.cuda.device(dev):
             return attention_packed(q, k, v, cu_seqlens, Hq, Hk, D, causal, cu_seqlens_k, out, workspace)
     if out is None:
@@ -458,10 +464,10 @@ def attention_prefill_paged(q: torch.Tensor, k_cache: torch.Tensor, v_cache: tor
     _ints(cu_seqlens, "cu_seqlens", B + 1)
     _ints(seq_lens, "seq_lens", B)
     ldo = Hq * D if out is None else _rows_of(out, "out", T, Hq * D, dt)
-    _check(workspace, "workspace", None, torch.uint8)
-    _need_gpu(q, k_cache, v_cache, cu_seqlens, block_table, seq_lens, out, workspace)
+    if workspace is not None:
+        _check(workspace, "workspace", None, torch.uint8)
     dev = q.device
-    if _elsewhere(dev):
+    if _elsewhere(q, k_cache, v_cache, cu_seqlens, block_table, seq_lens, out, workspace):
         with torch.cuda.device(dev):
             return attention_prefill_paged(q, k_cache, v_cache, cu_seqlens, block_table, seq_lens, Hq, causal, out,
                                            workspace)
@@ -502,10 +508,10 @@ def attention_decode(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
     ldq = _rows_of(q, "q", B, Hq * D, dt)
     _ints(seq_lens, "seq_lens", B)
     ldo = Hq * D if out is None else _rows_of(out, "out", B, Hq * D, dt)
-    _check(workspace, "workspace", None, torch.uint8)
-    _need_gpu(q, k_cache, v_cache, block_table, seq_lens, out, workspace)
+    if workspace is not None:
+        _check(workspace, "workspace", None, torch.uint8)
     dev = q.device
-    if _elsewhere(dev):
+    if _elsewhere(q, k_cache, v_cache, block_table, seq_lens, out, workspace):
         with torch.cuda.device(dev):
             return attention_decode(q, k_cache, v_cache, block_table, seq_lens, Hq, max_len, out, workspace)
     if max_len is None:
