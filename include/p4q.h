@@ -303,13 +303,13 @@ int p4q_attention_prefill(p4q_dtype dt, int B, int L, int H, int D,
  *   the call splits the keys of a row among work-groups, without it the call
  *   runs unsplit, and the two agree within the rounding of fp32 sums.  Nothing
  *   of it is read before the call has written it.
- *   p4q_attention_decode_workspace_bytes: required where nonzero, 16-byte
- *   aligned; its first 32768 bytes hold arrival counters, which must be zero
- *   before the first call and are zero again after each.  Calls that share a
- *   workspace must not overlap.  Both sizes depend on the current device.
- *   A sequence's result does not depend on the order in which its parts finish.
- * Limits: T, B >= 1, T <= 2^24, B <= 65535, Tk >= 0, Hq <= 1024, T Hq / Hk <
- *   2^31, max_pages * page_size < 2^30; row strides >= heads * D, multiples of 8
+ *   p4q_attention_decode_workspace_bytes: required, 16-byte aligned; its first
+ *   32768 bytes hold arrival counters, which must be zero before the first
+ *   call and are zero again after each.  Calls that share a workspace must not
+ *   overlap.  Both sizes depend on the current device.
+ *   Results do not depend on the order in which parts of a call finish.
+ * Limits: T, B >= 1, T <= 2^24, B <= 65535, 0 <= Tk <= 2^24, Hq <= 1024,
+ *   T Hq / Hk < 2^31, T Hq / 128 + B Hk < 2^26, max_pages * page_size < 2^30; row strides >= heads * D, multiples of 8
  *   and < 2^24; rope_base > 1; data pointers 16-byte aligned, int32 pointers
  *   4-byte aligned.
  * ---------------------------------------------------------------------- */

@@ -482,13 +482,13 @@ def attention_prefill_paged(q: torch.Tensor, k_cache: torch.Tensor, v_cache: tor
     return out
 
 
-def attention_decode_workspace(B: int, Hq: int, Hk: int, D: int, max_len: int, device) -> Optional[torch.Tensor]:
-    """Workspace for attention_decode(), or None where it needs none.  Its head
-    holds arrival counters that start at zero (every call leaves them zero again)."""
+def attention_decode_workspace(B: int, Hq: int, Hk: int, D: int, max_len: int, device) -> torch.Tensor:
+    """Workspace for attention_decode().  Its head holds arrival counters that start
+    at zero (every call leaves them zero again)."""
     with torch.cuda.device(device):
         n = lib().p4q_attention_decode_workspace_bytes(B, Hq, Hk, D, max_len)
         if n == 0:
-            return None
+            raise P4QError(P4Q_ERR_INVALID_ARG, f"unsupported decode shape B={B} Hq={Hq} Hk={Hk} D={D} max_len={max_len}")
         ws = torch.empty(n, dtype=torch.uint8, device=device)
         ws[:32768].zero_()
         return ws
@@ -500,9 +500,9 @@ def attention_decode(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
     """Attention of one new token per sequence over a paged cache
     (p4q_attention_decode): q [B, >= Hq*D], seq_lens int32 [B] (keys of each
     sequence, the new one included; 0: zeros), max_len a bound of them (default:
-    what a row of block_table holds).  Without `workspace` the call makes one if it
-    needs one; a given one must come from attention_decode_workspace() and serve one
-    call at a time.  Returns out [B, Hq*D]."""
+    what a row of block_table holds).  Without `workspace` the call makes one (and
+    clears its counters); a given one must come from attention_decode_workspace() and
+    serve one call at a time.  Returns out [B, Hq*D]."""
     pages, Hk, page, D, B, width = _cache_shape(k_cache, v_cache, block_table, q, Hq)
     dt = q.dtype
     ldq = _rows_of(q, "q", B, Hq * D, dt)
@@ -522,8 +522,8 @@ def attention_decode(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
         workspace = attention_decode_workspace(B, Hq, Hk, D, max_len, dev)
     check(lib().p4q_attention_decode(
         _dtype_code(dt), B, Hq, Hk, D, _ptr(q), ldq, _ptr(k_cache), _ptr(v_cache), pages, page, _ptr(block_table),
-        width, _ptr(seq_lens), max_len, _ptr(out), ldo, _ptr(workspace),
-        0 if workspace is None else workspace.numel(), _stream(dev)))
+        width, _ptr(seq_lens), max_len, _ptr(out), ldo, _ptr(workspace), workspace.numel(),
+        _stream(dev)))
     return out
 
 

@@ -115,7 +115,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_decode_attention(DecodeAtten
     int64_t all = 0;
     for (int i = 0; i < a.B; i += 64) {
         const int n = i + lane < a.B ? tiles_of(a.lens[i + lane]) : 0;
-        all += __builtin_amdgcn_readlane((int)wave_inclusive_scan((uint32_t)n), 63);
+        all += (uint32_t)__builtin_amdgcn_readlane((int)wave_inclusive_scan((uint32_t)n), 63);
     }
     all *= heads;
     Shares shares;
@@ -139,17 +139,17 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_decode_attention(DecodeAtten
         int64_t before = 0;
         for (int i = 0; i < a.B; i += 64) {
             const int n = i + lane < a.B ? tiles_of(a.lens[i + lane]) : 0;
-            const int upto = (int)wave_inclusive_scan((uint32_t)n);
+            const uint32_t upto = wave_inclusive_scan((uint32_t)n);
             const int k = __popcll(__ballot(before + upto <= want));
             if (k < 64) {                       // (a sequence: want < all / heads)
                 b = i + k;
                 tiles = __builtin_amdgcn_readlane(n, k);
-                const int64_t at = p - (before + __builtin_amdgcn_readlane(upto, k) - tiles) * heads;
+                const int64_t at = p - (before + (uint32_t)__builtin_amdgcn_readlane((int)upto, k) - tiles) * heads;
                 hb = (int)div_floor(at, tiles);
                 r = (int)(at - (int64_t)hb * tiles);
                 break;
             }
-            before += __builtin_amdgcn_readlane(upto, 63);
+            before += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
         }
     }
 
@@ -438,7 +438,6 @@ int64_t decode_groups(int B, int Hq, int Hk, int max_len) {
 }  // namespace
 
 size_t decode_attention_workspace_bytes(int B, int Hq, int Hk, int D, int max_len) {
-    if (max_len <= kRound) return 0;                                        // a round: nothing to split
     return kArrivalBytes + (size_t)(2 * decode_groups(B, Hq, Hk, max_len) * kCols * (D + 2)) * 4;
 }
 

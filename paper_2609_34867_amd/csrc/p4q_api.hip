@@ -293,7 +293,8 @@ static int check_heads(const char *who, p4q_dtype dt, int T, int B, int Hq, int 
         return fail(P4Q_ERR_INVALID_ARG, "%s: T=%d B=%d Hq=%d Hk=%d D=%d (positive, Hq a multiple of Hk)", who, T, B,
                     Hq, Hk, D);
     if (D != 64 && D != 128) return fail(P4Q_ERR_UNSUPPORTED, "%s: head dimension %d (64 or 128)", who, D);
-    if (T > (1 << 24) || B > 65535 || Hq > 1024 || (int64_t)T * (Hq / Hk) >= (1LL << 31))
+    if (T > (1 << 24) || B > 65535 || Hq > 1024 || (int64_t)T * (Hq / Hk) >= (1LL << 31) ||
+        (int64_t)T * Hq / 128 + (int64_t)B * Hk >= (1LL << 26))
         return fail(P4Q_ERR_UNSUPPORTED, "%s: T=%d B=%d Hq=%d Hk=%d too large", who, T, B, Hq, Hk);
     return P4Q_OK;
 }
@@ -435,9 +436,9 @@ int p4q_attention_decode(p4q_dtype dt, int B, int Hq, int Hk, int D, const void 
         return fail(P4Q_ERR_INVALID_ARG, "%s: max_len=%d outside [1, %lld]", who, max_len,
                     (long long)max_pages * page_size);
     const size_t need = p4q::decode_attention_workspace_bytes(B, Hq, Hk, D, max_len);
-    if (need > 0 && (!ws || ws_bytes < need))
+    if (!ws || ws_bytes < need)
         return fail(P4Q_ERR_WORKSPACE, "%s: workspace %zu < %zu bytes", who, ws_bytes, need);
-    if (need > 0 && !aligned(ws, 16)) return fail(P4Q_ERR_INVALID_ARG, "%s: workspace not 16-byte aligned", who);
+    if (!aligned(ws, 16)) return fail(P4Q_ERR_INVALID_ARG, "%s: workspace not 16-byte aligned", who);
     p4q::DecodeAttention a{};
     a.B = B, a.Hq = Hq, a.Hk = Hk, a.max_len = max_len;
     a.q = static_cast<const uint16_t *>(q), a.k = static_cast<const uint16_t *>(k_cache);

@@ -103,7 +103,7 @@ __device__ __forceinline__ RowTile find_tile(const PromptAttention &a, int x, in
     }
     if (t.b < 0) return t;
     const int last = min(t.r0 + kQB, t.rows) - 1;
-    const int keys = CAUSAL ? min(t.cap, max(0, by_g(last) + 1 + t.m - t.n)) : t.cap;
+    const int keys = CAUSAL ? min(t.cap, max(0, by_g(last) + 1 + (t.m - t.n))) : t.cap;
     t.ntiles = (keys + kKT - 1) / kKT;
     t.splits = max(1, min(min(a.splits, t.ntiles / kSplitTiles), (int)__builtin_sqrtf((float)t.ntiles * a.split_gain)));
     return t;
@@ -438,7 +438,7 @@ __global__ __launch_bounds__(256) void k_prompt_join(PromptAttention a) {
             o.w = o.w * f + x.w * e;
         }
         const int i = magic_div(row, a.g_magic, a.g_shift), h = hk * a.G + (row - i * a.G);
-        const int seen = CAUSAL ? i + 1 + t.m - t.n : t.m;
+        const int seen = CAUSAL ? i + 1 + (t.m - t.n) : t.m;
         const float inv = 1.0f / l;
         uint2 w = make_uint2(pack2_scaled<BF16>(o.x, o.y, inv), pack2_scaled<BF16>(o.z, o.w, inv));
         if (seen <= 0) w = make_uint2(0, 0);

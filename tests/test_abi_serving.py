@@ -53,7 +53,7 @@ HEADS = [(dict(dt=7), UNSUPPORTED), (dict(B=0), BAD), (dict(Hq=0), BAD), (dict(H
          (dict(D=0), BAD), (dict(D=96), UNSUPPORTED), (dict(B=65536), UNSUPPORTED),
          (dict(Hq=1026, ldq=1026 * 64), UNSUPPORTED), (dict(q=None), BAD), (dict(q=P + 8), BAD), (dict(ldq=248), BAD),
          (dict(ldq=260), BAD), (dict(ldq=1 << 24), UNSUPPORTED)]
-ROWS = [(dict(T=0), BAD), (dict(T=-1), BAD), (dict(T=(1 << 24) + 1), UNSUPPORTED), (dict(cu=None), BAD), (dict(cu=P + 2), BAD)]
+ROWS = [(dict(T=0), BAD), (dict(T=-1), BAD), (dict(T=(1 << 24) + 1), UNSUPPORTED), (dict(T=1 << 24, Hq=1024, Hk=1024), UNSUPPORTED), (dict(cu=None), BAD), (dict(cu=P + 2), BAD)]
 KEYS = [(dict(k=None), BAD), (dict(v=None), BAD), (dict(k=P + 2), BAD), (dict(v=P + 8), BAD), (dict(ldk=64), BAD),
         (dict(ldv=132), BAD), (dict(ldk=1 << 24), UNSUPPORTED)]
 CACHE = [(dict(kc=None), BAD), (dict(vc=None), BAD), (dict(kc=P + 8), BAD), (dict(table=None), BAD), (dict(table=P + 1), BAD),
@@ -90,7 +90,7 @@ def test_paged_refusals(kw, status):
 
 @pytest.mark.parametrize("kw,status", HEADS + CACHE + OUT + [
     (dict(lens=None), BAD), (dict(lens=P + 2), BAD), (dict(max_len=0), BAD), (dict(max_len=65), BAD),
-    (dict(max_len=4096, width=256), ROOM), (dict(max_len=4096, width=256, ws=P, ws_bytes=100), ROOM),
+    (dict(), ROOM), (dict(max_len=1), ROOM), (dict(max_len=4096, width=256), ROOM), (dict(max_len=4096, width=256, ws=P, ws_bytes=100), ROOM),
     (dict(max_len=4096, width=256, ws=P + 8, ws_bytes=1 << 30), BAD)])
 def test_decode_refusals(kw, status):
     refused(decode, kw, status)
@@ -109,6 +109,14 @@ def test_prompt_workspace_extremes(args):
                                   (1, 4, 3, 64, 64), (1, 4, 4, 96, 4096), (1, 4, 4, 64, 0), (1, 4, 4, 64, 1 << 30)])
 def test_decode_workspace_extremes(args):
     assert L.lib().p4q_attention_decode_workspace_bytes(*args) == 0
+
+
+@pytest.mark.parametrize("B,Hq,Hk,D,max_len", [(1, 1, 1, 64, 1), (5, 2, 2, 128, 100), (65535, 16, 1, 64, 128), (64, 64, 8, 128, 1 << 29)])
+def test_every_decode_call_has_room_for_two_parts_of_each_share(B, Hq, Hk, D, max_len):
+    """Short calls too: a work-group's share may begin and end within a sequence."""
+    n = L.lib().p4q_attention_decode_workspace_bytes(B, Hq, Hk, D, max_len)
+    groups = min(512, B * Hk * -(-(Hq // Hk) // 16) * -(-max_len // 128))     # of 256 compute units
+    assert n >= 32768 + 2 * groups * 16 * (D + 2) * 4
 
 
 def test_workspaces_where_keys_are_split():

@@ -444,6 +444,26 @@ def test_decode_split_over_long_keys(dtype, Hq, Hk, D):
     decode_case(73, dtype, Hq, Hk, D, 16, [9001], width=2048)
 
 
+@pytest.mark.parametrize("B,Hq,Hk,D,most", [(5, 2, 2, 128, 100), (3, 40, 4, 64, 60), (70, 24, 24, 64, 120), (70, 24, 12, 128, 128),
+                                            (200, 16, 16, 64, 1), (130, 5, 5, 64, 33)])
+def test_decode_short_keys_shared_unevenly(B, Hq, Hk, D, most):
+    """Short sequences of different lengths, fewer and more of them than
+    work-groups: their shares begin and end within sequences, and all sums of
+    parts stay in the workspace."""
+    lens = [(37 * i) % (most + 1) for i in range(B - 1)] + [most]
+    g = gen(79)
+    kc, vc, table = make_cache(g, "fp16", lens, Hk, D, 16)
+    q = randn(g, "fp16", B, Hq * D)
+    n = p4q.attention_decode_workspace(B, Hq, Hk, D, most, dev()).numel()
+    ws = Guarded((n,), torch.uint8, "workspace")
+    ws.t.zero_()
+    out = p4q.attention_decode(q, kc, vc, table, ints(lens), Hq, max_len=most, workspace=ws.t)
+    ws.check()
+    assert not ws.t[:32768].any()
+    tab, k64, v64 = table.cpu().numpy(), f64(kc), f64(vc)
+    check_attention(out, q, lambda b: tuple(oracle.cache_rows(c, tab[b], lens[b]) for c in (k64, v64)), [1] * B, Hq, D, "fp16")
+
+
 @pytest.mark.parametrize("dtype", ["fp16", "bf16"])
 def test_decode_large_logits(dtype):
     decode_case(74, dtype, 4, 1, 128, 16, [500, 3000], std=8.0)
