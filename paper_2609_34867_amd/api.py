@@ -296,6 +296,10 @@ def attention_prefill(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, B: int,
 
 
 # --------------------------------------------------------------------------- serving
+# (called for every layer of every token: the checks take care to be quick)
+_CODES = {torch.float16: P4Q_FP16, torch.bfloat16: P4Q_BF16}
+
+
 def _rows_of(t: torch.Tensor, name: str, rows: int, cols: int, dtype) -> int:
     """Checks a 2-D operand [rows, >= cols], whose rows may be columns of a wider
     buffer, and returns its row stride (a single row may have any: its width)."""
@@ -330,7 +334,7 @@ def _ints(t: Optional[torch.Tensor], name: str, n: int) -> None:
 
 def _cache_shape(k_cache: torch.Tensor, v_cache: torch.Tensor, block_table: torch.Tensor, q: torch.Tensor, Hq: int):
     """(pages, Hk, page size, D, B, table width) of a paged cache and its table."""
-    if q.dtype not in _F16:
+    if q.dtype not in _CODES:
         raise ValueError(f"q must be fp16 or bf16, got {q.dtype}")
     shape = k_cache.shape
     if len(shape) != 4 or shape != v_cache.shape:
@@ -383,9 +387,9 @@ def rope_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqlens: t
     if q_out is None:
         q_out, ldqo = torch.empty((T, Hq * D), dtype=dt, device=dev), Hq * D
     check(lib().p4q_rope_append(
-        _dtype_code(dt), T, B, Hq, Hk, D, _ptr(q), ldq, _ptr(k), ldk, _ptr(v), ldv, _ptr(cu_seqlens),
-        _ptr(cache_lens), _ptr(positions), rope_base, _ptr(q_out), ldqo, _ptr(k_out), ldko, _ptr(k_cache),
-        _ptr(v_cache), pages, page, _ptr(block_table), width, _stream(dev)))
+        _CODES[dt], T, B, Hq, Hk, D, q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, cu_seqlens.data_ptr(),
+        _ptr(cache_lens), _ptr(positions), rope_base, q_out.data_ptr(), ldqo, _ptr(k_out), ldko, k_cache.data_ptr(),
+        v_cache.data_ptr(), pages, page, block_table.data_ptr(), width, _stream(dev)))
     return q_out, k_out
 
 
@@ -418,7 +422,7 @@ def attention_packed(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqle
     likewise for the keys (default: cu_seqlens).  Causal: a sequence's last token
     sees its last key.  Returns out [T, Hq*D]; tokens that see no key get zeros,
     rows behind the last sequence are left as they were."""
-    if q.dtype not in _F16:
+    if q.dtype not in _CODES:
         raise ValueError(f"q must be fp16 or bf16, got {q.dtype}")
     T, Tk, dt = q.shape[0], k.shape[0], q.dtype
     ldq = _rows_of(q, "q", T, Hq * D, dt)
@@ -443,8 +447,8 @@ def attention_packed(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqle
     if workspace is None:
         workspace = _own_prompt_workspace(T, B, Hq, Hk, D, Tk, dev)
     check(lib().p4q_attention_packed(
-        _dtype_code(dt), T, Tk, B, Hq, Hk, D, _ptr(q), ldq, _ptr(k), ldk, _ptr(v), ldv, _ptr(cu_seqlens),
-        _ptr(cu_seqlens_k), _ptr(out), ldo, int(causal), _ptr(workspace),
+        _CODES[dt], T, Tk, B, Hq, Hk, D, q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, cu_seqlens.data_ptr(),
+        _ptr(cu_seqlens_k), out.data_ptr(), ldo, int(causal), _ptr(workspace),
         0 if workspace is None else workspace.numel(), _stream(dev)))
     return out
 
@@ -476,8 +480,8 @@ def attention_prefill_paged(q: torch.Tensor, k_cache: torch.Tensor, v_cache: tor
     if workspace is None:
         workspace = _own_prompt_workspace(T, B, Hq, Hk, D, width * page, dev)
     check(lib().p4q_attention_prefill_paged(
-        _dtype_code(dt), T, B, Hq, Hk, D, _ptr(q), ldq, _ptr(k_cache), _ptr(v_cache), pages, page,
-        _ptr(block_table), width, _ptr(cu_seqlens), _ptr(seq_lens), _ptr(out), ldo, int(causal), _ptr(workspace),
+        _CODES[dt], T, B, Hq, Hk, D, q.data_ptr(), ldq, k_cache.data_ptr(), v_cache.data_ptr(), pages, page,
+        block_table.data_ptr(), width, cu_seqlens.data_ptr(), seq_lens.data_ptr(), out.data_ptr(), ldo, int(causal), _ptr(workspace),
         0 if workspace is None else workspace.numel(), _stream(dev)))
     return out
 
@@ -521,8 +525,8 @@ def attention_decode(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
     if workspace is None:
         workspace = attention_decode_workspace(B, Hq, Hk, D, max_len, dev)
     check(lib().p4q_attention_decode(
-        _dtype_code(dt), B, Hq, Hk, D, _ptr(q), ldq, _ptr(k_cache), _ptr(v_cache), pages, page, _ptr(block_table),
-        width, _ptr(seq_lens), max_len, _ptr(out), ldo, _ptr(workspace), workspace.numel(),
+        _CODES[dt], B, Hq, Hk, D, q.data_ptr(), ldq, k_cache.data_ptr(), v_cache.data_ptr(), pages, page, block_table.data_ptr(),
+        width, seq_lens.data_ptr(), max_len, out.data_ptr(), ldo, _ptr(workspace), workspace.numel(),
         _stream(dev)))
     return out
 
