@@ -285,7 +285,7 @@ int p4q_attention_prefill(p4q_dtype dt, int B, int L, int H, int D,
  *     or every j < m (causal = 0),
  *   out[i, h] = sum_j softmax_j(S) v[j, h / (Hq / Hk)];  zeros without a key.
  * Arithmetic as p4q_attention_prefill.  A non-finite value row may also reach
- * tokens whose mask ends less than 32 keys before it.
+ * tokens whose mask ends less than 64 keys before it.
  *
  * p4q_attention_prefill_paged: the same with the m = seq_lens[b] keys of the
  * cache (int32 [B]; the call's own tokens included, appended before).

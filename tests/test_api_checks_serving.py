@@ -98,3 +98,54 @@ def test_decode_checks():
     raises("seq_lens must be", api.attention_decode, f16(2, 256), KC, VC, TABLE, LENS.long(), 4)
     raises("out must have shape", api.attention_decode, *ok, out=f16(2, 128))
     raises("workspace must be", api.attention_decode, *ok, workspace=f16(6))
+
+
+# ------------------------------------------------------------------ another device than the current one
+class Recorder:
+    """Stands in for the library: keeps what each call is given."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        def call(*a):
+            self.calls.append((name, a))
+            return 4096 if name.endswith("_bytes") else 0
+        return call
+
+
+def test_calls_on_another_device_pass_everything_on(monkeypatch):
+    """Tensors of a device that is not current: the call is made again, with that
+    device current and the same arguments."""
+    from contextlib import contextmanager
+    rec, entered = Recorder(), []
+
+    @contextmanager
+    def device(d):
+        entered.append(d)
+        yield
+
+    monkeypatch.setattr(api, "lib", lambda: rec)
+    monkeypatch.setattr(api, "_stream", lambda d: 7)
+    monkeypatch.setattr(api.torch.cuda, "device", device)
+    ws = torch.zeros(4096, dtype=torch.uint8)
+    calls = [
+        lambda: api.rope_append(Q, K, V, CU, TABLE, KC, VC, 4, cache_lens=LENS, positions=i32(6), rope_base=5e5,
+                                q_out=f16(6, 256), k_out=f16(6, 128)),
+        lambda: api.attention_packed(Q, f16(9, 128), f16(9, 128), CU, 4, 2, 64, causal=False, cu_seqlens_k=CU,
+                                     out=f16(6, 256), workspace=ws),
+        lambda: api.attention_prefill_paged(Q, KC, VC, CU, TABLE, LENS, 4, causal=False, out=f16(6, 256), workspace=ws),
+        lambda: api.attention_decode(f16(2, 256), KC, VC, TABLE, LENS, 4, max_len=33, out=f16(2, 256), workspace=ws),
+    ]
+    for call in calls:
+        got = []
+        for away in (False, True):
+            answers = [away, False]                       # not current, then current
+            monkeypatch.setattr(api, "_elsewhere", lambda *t: answers.pop(0))
+            rec.calls.clear()
+            entered.clear()
+            call()
+            assert entered == ([torch.device("cpu")] if away else [])
+            # (addresses of the tensors made in each call differ)
+            got.append([(n, [x for x in a if not (isinstance(x, int) and x > 1 << 20)]) for n, a in rec.calls])
+        assert got[0] == got[1] and len(got[0]) == 1

@@ -296,7 +296,8 @@ def test_packed_sequences_do_not_meet():
 
 def test_packed_masked_keys_and_values_do_not_leak():
     """Keys past a token's mask: non-finite keys reach no earlier token at all,
-    non-finite values none whose mask ends 32 or more keys before them."""
+    non-finite values none whose mask ends 64 or more keys before them (here, with
+    rows and keys aligned, 32)."""
     Hq, Hk, D, n = 2, 1, 128, 200
     g = gen(49)
     q, k, v = randn(g, "bf16", n, Hq * D), randn(g, "bf16", n, D), randn(g, "bf16", n, D)
@@ -309,6 +310,24 @@ def test_packed_masked_keys_and_values_do_not_leak():
         out = p4q.attention_packed(q, k, v2, cu_of([n]), Hq, Hk)
         assert torch.equal(out[:max(0, row - 32)], ref[:max(0, row - 32)])
         assert not torch.isfinite(out[row:]).any()
+
+
+@pytest.mark.parametrize("more", [1, 17, 33, 63])
+@pytest.mark.parametrize("Hq,Hk", [(1, 1), (2, 1), (3, 1)])
+def test_packed_masked_values_do_not_leak_in_a_chunk(Hq, Hk, more):
+    """The same where the tokens follow `more` earlier keys, so that the ends of
+    masks, rows and tiles fall anywhere."""
+    D, n = 64, 150
+    g = gen(52)
+    q, k, v = randn(g, "fp16", n, Hq * D), randn(g, "fp16", n + more, D), randn(g, "fp16", n + more, D)
+    args = (cu_of([n]), Hq, Hk, D)
+    ref = p4q.attention_packed(q, k, v, *args, cu_seqlens_k=cu_of([n + more]))
+    for j in (more, more + 31, more + 66, n + more - 1):                   # seen from token j - more on
+        v2 = v.clone()
+        v2[j] = float("nan")
+        out = p4q.attention_packed(q, k, v2, *args, cu_seqlens_k=cu_of([n + more]))
+        clean = max(0, j - more - 63)
+        assert torch.equal(out[:clean], ref[:clean]) and torch.isnan(out[j - more:]).all()
 
 
 def test_packed_bad_lists_stay_inside():
