@@ -38,7 +38,8 @@
 // rows and keys) and 1.8 per tile.  One of 371 tokens, 40 heads: 13.6 us, six tiles one after the
 // other at 1.3 each.  Not kept, none faster: three tiles in flight; two key halves per row tile
 // in one work-group (371 tokens 14.5 us); sequences in order of length (4 of 300 to 4000
-// tokens, D = 64: 102 for 93 us); four wavefronts per SIMD at D = 64 (spills).
+// tokens, D = 64: 102 for 93 us).  D = 64 runs four wavefronts per SIMD (128 registers, 40
+// sequences of 577 tokens, 20 heads, 110 us; three of them 117).
 #include "attention_device.h"
 #include "gemm_device.h"
 #include "kv_cache.h"
@@ -120,7 +121,7 @@ __device__ __forceinline__ RowTile find_tile(const PromptAttention &a, int x, in
 }
 
 template <bool BF16, int D, bool CAUSAL, bool PAGED>
-__global__ __launch_bounds__(64 * kNW, D == 64 ? 3 : 2) void k_prompt_attention(PromptAttention a) {
+__global__ __launch_bounds__(64 * kNW, D == 64 ? 4 : 2) void k_prompt_attention(PromptAttention a) {
     constexpr int kRow = 2 * D;             // bytes of a K or V row
     constexpr int kOperand = kKT * kRow;
     constexpr int kTile = 2 * kOperand;     // K, then V
@@ -275,12 +276,16 @@ __global__ __launch_bounds__(64 * kNW, D == 64 ? 3 : 2) void k_prompt_attention(
             if (i + 2 < kSteps / 2) k_batch(i + 2);
             __builtin_amdgcn_sched_barrier(0);
         }
-        // V^T of the first 64 values: in flight during the softmax
+        // V^T of the first 64 values: in flight during the softmax (D = 64: behind it,
+        // for the registers that a fourth wavefront per SIMD needs)
         uint4 vf[2][2 * NH];
+        auto v_first = [&]() __attribute__((always_inline)) {
 #pragma unroll
-        for (int db = 0; db < 2; ++db)
+            for (int db = 0; db < 2; ++db)
 #pragma unroll
-            for (int s = 0; s < 2 * NH; ++s) vf[db][s] = v_read(db, s);
+                for (int s = 0; s < 2 * NH; ++s) vf[db][s] = v_read(db, s);
+        };
+        if constexpr (D == 128) v_first();
         issue(true, kt + 1, next_page);
         __builtin_amdgcn_sched_barrier(0);
         // mask (only where the tile reaches past what every row sees; one
@@ -329,6 +334,7 @@ __global__ __launch_bounds__(64 * kNW, D == 64 ? 3 : 2) void k_prompt_attention(
         }
         lsum += psum;                                       // this lane's half; joined at the end
         __builtin_amdgcn_sched_barrier(0);
+        if constexpr (D == 64) v_first();
         // O^T += V^T P^T (steps of 16 keys), each block's operands read two
         // blocks ahead
 #pragma unroll
