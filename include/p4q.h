@@ -261,8 +261,10 @@ int p4q_attention_prefill(p4q_dtype dt, int B, int L, int H, int D,
  * nothing out of range: a token whose place has no page in the cache is not
  * appended, and a query that sees a key without one (an entry outside
  * [0, num_pages), a length past the table or past max_len) gets NaN.
- * Negative lengths count as 0.  cu_seqlens that do not ascend, or that leave the
- * rows, are cut to them.
+ * Negative seq_lens count as 0; after negative cache_lens a sequence's tokens have
+ * negative places, which no page holds, up to its place 0.  cu_seqlens that do not
+ * ascend, or that leave the rows, stay inside them; which sequence a row then counts
+ * to is not defined.
  *
  * p4q_rope_append: token t, the i-th of sequence b in this call, takes place
  * s = cache_lens[b] + i in its sequence (cache_lens int32 [B]: keys cached
@@ -309,9 +311,9 @@ int p4q_attention_prefill(p4q_dtype dt, int B, int L, int H, int D,
  *   overlap.  Both sizes depend on the current device.
  *   Results do not depend on the order in which parts of a call finish.
  * Limits: T, B >= 1, T <= 2^24, B <= 65535, 0 <= Tk <= 2^24, Hq <= 1024,
- *   T Hq / Hk < 2^31, T Hq / 128 + B Hk < 2^26, max_pages * page_size < 2^30; row strides >= heads * D, multiples of 8
- *   and < 2^24; rope_base > 1; data pointers 16-byte aligned, int32 pointers
- *   4-byte aligned.
+ *   T Hq / Hk < 2^31, T Hq / 128 + B Hk < 2^26, max_pages * page_size < 2^30;
+ *   row strides >= heads * D, multiples of 8 and < 2^24; rope_base > 1; data
+ *   pointers 16-byte aligned, int32 pointers 4-byte aligned.
  * ---------------------------------------------------------------------- */
 int p4q_rope_append(p4q_dtype dt, int T, int B, int Hq, int Hk, int D, const void *q, int64_t ldq,
                     const void *k, int64_t ldk, const void *v, int64_t ldv,
