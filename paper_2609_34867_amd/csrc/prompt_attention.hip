@@ -57,6 +57,7 @@ constexpr int kQW = 32;                 // rows per wavefront
 constexpr int kQB = kNW * kQW;          // rows per work-group
 constexpr int kKT = 64;                 // keys per tile
 constexpr float kRescale = 8.0f;        // raise the running max past this margin (exp2 units)
+constexpr float kFar = 1024.0f;         // largest maximum (exp2 units) whose rounding costs a weight less than 2^-14
 constexpr int kSplitTiles = 4;          // a split has at least this many tiles (if the row tile has)
 constexpr int kMaxSplits = 32;
 
@@ -316,7 +317,20 @@ __global__ __launch_bounds__(64 * kNW, D == 64 ? 4 : 2) void k_prompt_attention(
 #pragma unroll
                 for (int r = 0; r < 16; ++r) acc[db][r] *= alpha;
         }
-        const float mc = (mx == -__builtin_huge_valf()) ? 0.0f : mx * a.c2 - kBias;
+        // A weight is one fma and exp2: s c2 - mc.  That mc is rounded scales a row's weights
+        // by 2^(up to |mc| 2^-24): nothing that shows while |mx| c2 <= kFar, but past 2^28 they
+        // overflow, or vanish.  From rows whose maximum is that far off it is taken off first
+        // (one wave-uniform branch; without it the call takes the same time, with a
+        // subtraction for every score 1 to 8% more).
+        const float off = __builtin_fmaxf(mx, -3.0e38f);    // (no score yet: all of them -inf)
+        const bool far = __builtin_fabsf(off) * a.c2 > kFar;
+        const float rest = far ? off : 0.0f, mc = (off - rest) * a.c2 - kBias;
+        if (__any((int)far)) {
+#pragma unroll
+            for (int hf = 0; hf < NH; ++hf)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) st[hf][r] -= rest;
+        }
         float psum = 0.0f;
         uint4 pb[NH][2];
 #pragma unroll

@@ -357,6 +357,43 @@ def test_packed_offsets_pass_32_bits():
     assert torch.equal(rows[:, 4 * D:], ref) and torch.equal(rows[:, :2 * D], q)
 
 
+def far_scores(dtype, D, scale, sign, rows, keys, Hq, Hk, seed):
+    """q [rows, Hq D] all sign 2^a, k [keys, Hk D] in rows of 2^b n with 1 <= n <= 255 and a + b = scale:
+    every score is D 2^scale n / sqrt(D), exact in fp32, and two different ones are 700 and more apart in
+    units of log 2, so that a row's result is the mean of the values of its largest scores."""
+    b = min(8, scale)
+    n = np.random.default_rng(seed).integers(1, 256, (keys, Hk))
+    k = np.repeat(n[:, :, None] * 2.0 ** b, D, axis=2).reshape(keys, Hk * D)
+    q = torch.full((rows, Hq * D), sign * 2.0 ** (scale - b), dtype=DT[dtype], device=dev())
+    return q, torch.from_numpy(k).to(dev()).to(DT[dtype]), randn(gen(seed), dtype, keys, Hk * D)
+
+
+def far_bound(O, A, dtype):
+    """Equal weights of the largest scores (rounded once each: eps / 2), fp32 sums, the output's rounding."""
+    eps = torch.finfo(DT[dtype]).eps
+    inner = (eps / 2 + 2.0 ** -20) * A
+    return inner + eps / 2 * (np.abs(O) + inner) + 2.0 ** -25
+
+
+@pytest.mark.parametrize("dtype,D,scale", [("fp16", 128, 6), ("fp16", 64, 15), ("fp16", 128, 19), ("fp16", 64, 23),
+                                           ("bf16", 128, 6), ("bf16", 64, 24), ("bf16", 128, 40), ("bf16", 64, 90)])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("lens,keys", [([150, 40], [150, 70]), ([3], [5000])])
+def test_packed_far_scores(dtype, D, scale, sign, lens, keys):
+    """Finite scores of any size, whole and split: 2^28 and more in units of log 2 among them, which
+    no fp32 product with log2(e) holds to within a weight's range."""
+    Hq, Hk = 4, 2
+    q, k, v = far_scores(dtype, D, scale, sign, sum(lens), sum(keys), Hq, Hk, 53)
+    for causal in (True, False):
+        out = f64(p4q.attention_packed(q, k, v, cu_of(lens), Hq, Hk, D, causal, cu_seqlens_k=cu_of(keys))).reshape(-1, Hq, D)
+        at = np.concatenate([[0], np.cumsum(lens)]), np.concatenate([[0], np.cumsum(keys)])
+        for b in range(len(lens)):
+            rows, cols = slice(at[0][b], at[0][b + 1]), slice(at[1][b], at[1][b + 1])
+            O, A = oracle.grouped_attention(f64(q)[rows].reshape(-1, Hq, D), f64(k)[cols].reshape(-1, Hk, D),
+                                            f64(v)[cols].reshape(-1, Hk, D), causal)
+            assert_within(out[rows], O, far_bound(O, A, dtype), f"sequence {b}")
+
+
 # ------------------------------------------------------------------ prompts over the cache
 def paged_case(seed, dtype, Hq, Hk, D, P, lens, key_lens, causal=True, pad=0, width=None):
     g = gen(seed)
