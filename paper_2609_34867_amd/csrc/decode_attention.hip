@@ -281,11 +281,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_decode_attention(DecodeAtten
 #pragma unroll
                 for (int j = 0; j < kV; ++j) acc[j] *= alpha;
             }
-            const float mc = (mx == -__builtin_huge_valf()) ? 0.0f : mx * a.c2 - kBias;
+            // The maximum is taken off before the product with c2: rounded after it, it would
+            // scale the weights by 2^(up to |mx| c2 2^-24), which overflows or vanishes past 2^28.
+            const float off = __builtin_fmaxf(mx, -3.0e38f);    // (no score yet: all of them -inf)
             float w[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                w[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[i >> 2][i & 3], a.c2, -mc));
+                w[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[i >> 2][i & 3] - off, a.c2, kBias));
                 sum += w[i];
             }
             const uint4 pb = make_uint4(pack2<BF16>(w[0], w[1]), pack2<BF16>(w[2], w[3]), pack2<BF16>(w[4], w[5]),

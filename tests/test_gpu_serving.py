@@ -569,6 +569,27 @@ def test_decode_nonfinite_keys_and_values():
     assert (out[0, [5, D + 5]] == float("inf")).all() and torch.isfinite(out).sum() == Hq * D - 2
 
 
+@pytest.mark.parametrize("dtype,D,scale", [("fp16", 128, 6), ("fp16", 64, 15), ("fp16", 128, 19), ("fp16", 64, 23),
+                                           ("bf16", 128, 6), ("bf16", 64, 24), ("bf16", 128, 40), ("bf16", 64, 90)])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("keys", [[40, 600], [9001]])
+def test_decode_far_scores(dtype, D, scale, sign, keys):
+    """Finite scores of any size (as test_packed_far_scores), in whole units and in parts."""
+    Hq, Hk, P = 4, 2, 64
+    kc, vc, table = make_cache(gen(84), dtype, keys, Hk, D, P, fill=0)
+    tab, want = table.cpu().numpy(), []
+    for b, m in enumerate(keys):
+        q, k, v = far_scores(dtype, D, scale, sign, len(keys), m, Hq, Hk, 85 + b)
+        for j in range(0, m, P):
+            n = min(P, m - j)
+            kc[tab[b, j // P], :, :n] = k[j:j + n].view(n, Hk, D).transpose(0, 1)
+            vc[tab[b, j // P], :, :n] = v[j:j + n].view(n, Hk, D).transpose(0, 1)
+        want.append(oracle.grouped_attention(f64(q)[:1].reshape(1, Hq, D), f64(k).reshape(m, Hk, D), f64(v).reshape(m, Hk, D)))
+    out = f64(p4q.attention_decode(q, kc, vc, table, ints(keys), Hq)).reshape(-1, Hq, D)
+    for b, (O, A) in enumerate(want):
+        assert_within(out[b:b + 1], O, far_bound(O, A, dtype), f"sequence {b}")
+
+
 def test_offsets_in_the_cache_pass_32_bits():
     """A cache of more than 2^31 elements: append to, attend over and decode from
     its last pages."""
