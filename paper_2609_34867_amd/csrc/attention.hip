@@ -60,6 +60,7 @@ constexpr int kRow = kD * 2;            // bytes of a K or V row
 constexpr int kOperand = kKT * kRow;    // 16 KB
 constexpr int kTile = 2 * kOperand;     // K, then V
 constexpr float kRescale = 8.0f;        // raise the running max past this margin (exp2 units)
+constexpr float kFar = 1024.0f;         // largest maximum (exp2 units) whose rounding costs a weight less than 2^-14
 
 // LDS placement of 16-byte chunk c of row r.  K: the rows that a fragment
 // read takes together (16 of them, one chunk) fall in distinct banks; V: the
@@ -234,7 +235,18 @@ __global__ __launch_bounds__(64 * kNW, 2) void k_attention(const uint16_t *__res
 #pragma unroll
                 for (int r = 0; r < 16; ++r) acc[db][r] *= alpha;
         }
-        const float mc = (m == -__builtin_huge_valf()) ? 0.0f : m * c2;
+        // m c2 is rounded, which scales a query's weights by 2^(up to |m| c2 2^-24): nothing that
+        // shows while |m| c2 <= kFar, but past 2^28 they overflow, or vanish.  From queries
+        // whose maximum is that far off it is taken off first (one wave-uniform branch).
+        const float off = __builtin_fmaxf(m, -3.0e38f);     // (no score yet: all of them -inf)
+        const bool far = __builtin_fabsf(off) * c2 > kFar;
+        const float rest = far ? off : 0.0f, mc = (off - rest) * c2;
+        if (__any((int)far)) {
+#pragma unroll
+            for (int hf = 0; hf < NH; ++hf)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) st[hf][r] -= rest;
+        }
         float psum = 0.0f;
         uint4 pb[NH][2];
 #pragma unroll

@@ -172,3 +172,27 @@ def test_rows_of_many_megabytes(L):
     wide.copy_(rows)
     out = p4q.attention_prefill(wide[:, :HD], wide[:, HD:2 * HD], wide[:, 2 * HD:], 1, H, True)
     assert torch.equal(out, ref)
+
+
+@pytest.mark.parametrize("dtype,scale", [("fp16", 6), ("fp16", 15), ("fp16", 19), ("fp16", 23), ("bf16", 24), ("bf16", 90)])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("causal", [True, False])
+def test_far_scores(dtype, scale, sign, causal):
+    """Finite scores of any size: q all sign 2^a, k in rows of 2^b n with 1 <= n <= 255 and a + b = scale, so
+    that every score is exact in fp32, two different ones are 1000 and more apart in units of log 2,
+    and a query's result is the mean of the values of its largest scores: weights rounded once (eps / 2),
+    fp32 sums, the output's rounding."""
+    L, H, b = 200, 2, min(8, scale)
+    rng, dt = np.random.default_rng(63), torch.float16 if dtype == "fp16" else torch.bfloat16
+    n = rng.integers(1, 256, (L, H))
+    q = np.full((L, H, D), sign * 2.0 ** (scale - b))
+    k = np.repeat(n[:, :, None] * 2.0 ** b, D, axis=2)
+    v = torch.from_numpy(rng.standard_normal((L, H * D))).to(dt)
+    t = torch.cat([torch.from_numpy(x).reshape(L, H * D).to(dt) for x in (q, k)] + [v], 1).cuda()
+    out = p4q.attention_prefill(t[:, :H * D], t[:, H * D:2 * H * D], t[:, 2 * H * D:], 1, H, causal)
+    O, A = oracle.grouped_attention(q, k, v.double().numpy().reshape(L, H, D), causal)
+    eps = torch.finfo(dt).eps
+    inner = (eps / 2 + 2.0 ** -20) * A
+    err = np.abs(out.double().cpu().numpy().reshape(L, H, D) - O)
+    wrong = int((~(err <= inner + eps / 2 * (np.abs(O) + inner) + 2.0 ** -25)).sum())
+    assert wrong == 0, f"{wrong} of {err.size} out of tolerance"
