@@ -42,7 +42,21 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     else return __builtin_bit_cast(uint32_t, __builtin_convertvector(v2f{lo, hi}, v2h));
 }
 
-// the same of lo * c and hi * c.  In fp16 the product is rounded once, straight
+// the same towards zero, of values that are not negative
+template <bool BF16>
+__device__ __forceinline__ uint32_t pack2_down(float lo, float hi) {
+    if constexpr (BF16) return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
+    else return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(lo, hi));
+}
+
+// and back
+template <bool BF16>
+__device__ __forceinline__ v2f unpack2(uint32_t x) {
+    if constexpr (BF16) return v2f{__uint_as_float(x << 16), __uint_as_float(x & 0xFFFF0000u)};
+    else return __builtin_convertvector(__builtin_bit_cast(v2h, x), v2f);
+}
+
+// pack2 of lo * c and hi * c.  In fp16 the product is rounded once, straight
 // to 16 bits (v_fma_mixlo_f16), which takes a conversion of its own for each: the
 // packed one is handed products that are already rounded to fp32.
 template <bool BF16>

@@ -21,9 +21,12 @@
 //    come by scalar loads: a vector load of the table would queue behind the values
 //    (one of 131071 keys: 147 us).
 // The softmax keeps a running maximum per query, raised only when a tile exceeds it
-// by more than 2^8 (exp2 units).  Weights are rounded to the cache's type before they
-// multiply v, which costs half a step of it per weight and lets the matrix
-// instructions take them; fp16 ones carry 2^7, so that they reach down to 2^-31 of the
+// by more than 2^8 (exp2 units).  The matrix instructions take weights of the cache's
+// type, so each goes in as two such numbers, its rounding and what that left out: within
+// 2^-15 (bf16) and 2^-21 (fp16) of itself, where one alone is off by 2^-8 and 2^-11 and
+// makes the outputs' error 1.3 times what rounding them costs.  Their products run under
+// the loads (64 ragged sequences 132 us, with one piece 129; one of 131071 keys 91.7 either
+// way).  fp16 weights carry 2^7, so that they reach down to 2^-31 of the
 // largest.  Scores, maxima, sums and the accumulated values are fp32.
 //
 // Work is dealt on the device, where the lengths are: all tiles of all units, in
@@ -109,6 +112,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_decode_attention(DecodeAtten
     constexpr int kBatch = 512 / D;             // parts per wavefront of the join at a time
     constexpr int kCoherent = 16;               // sc1: past the caches that other XCDs do not see
     constexpr float kBias = BF16 ? 0.0f : 7.0f;
+    constexpr float kLeast = BF16 ? 0x1p-100f : 0x1p-24f;   // (a weight of 0 becomes this: 2^-31 of the largest)
     __shared__ __attribute__((aligned(16))) float s_acc[kWaves][kCols * kRow];
     __shared__ float s_max[kWaves][kCols], s_sum[kWaves][kCols];
     __shared__ int s_last;
@@ -290,16 +294,30 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_decode_attention(DecodeAtten
                 w[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[i >> 2][i & 3] - off, a.c2, kBias));
                 sum += w[i];
             }
-            const uint4 pb = make_uint4(pack2<BF16>(w[0], w[1]), pack2<BF16>(w[2], w[3]), pack2<BF16>(w[4], w[5]),
-                                        pack2<BF16>(w[6], w[7]));
+            // Each weight as a sum of two 16-bit numbers: the first cut off, not rounded, and
+            // the second never 0, so that neither turns an infinite value into NaN.
+            uint32_t hi[4], lo[4];
 #pragma unroll
-            for (int j = 0; j < kV; ++j) {
-                const uint32_t sel = (j & 1) ? 0x07060302u : 0x05040100u;
-                const uint4 va = make_uint4(__builtin_amdgcn_perm(vf[1][j >> 1], vf[0][j >> 1], sel),
-                                            __builtin_amdgcn_perm(vf[3][j >> 1], vf[2][j >> 1], sel),
-                                            __builtin_amdgcn_perm(vf[5][j >> 1], vf[4][j >> 1], sel),
-                                            __builtin_amdgcn_perm(vf[7][j >> 1], vf[6][j >> 1], sel));
-                acc[j] = mfma16<BF16>(va, pb, acc[j]);
+            for (int i = 0; i < 4; ++i) {
+                hi[i] = pack2_down<BF16>(w[2 * i], w[2 * i + 1]);
+                const v2f h = unpack2<BF16>(hi[i]);
+                lo[i] = pack2<BF16>(__builtin_fmaxf(w[2 * i] - h[0], kLeast), __builtin_fmaxf(w[2 * i + 1] - h[1], kLeast));
+            }
+            const uint4 ph = make_uint4(hi[0], hi[1], hi[2], hi[3]), pl = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+            // (the second pieces one step behind the first, whose sums they wait for)
+            uint4 va, last;
+#pragma unroll
+            for (int j = 0; j <= kV; ++j) {
+                if (j < kV) {
+                    const uint32_t sel = (j & 1) ? 0x07060302u : 0x05040100u;
+                    va = make_uint4(__builtin_amdgcn_perm(vf[1][j >> 1], vf[0][j >> 1], sel),
+                                    __builtin_amdgcn_perm(vf[3][j >> 1], vf[2][j >> 1], sel),
+                                    __builtin_amdgcn_perm(vf[5][j >> 1], vf[4][j >> 1], sel),
+                                    __builtin_amdgcn_perm(vf[7][j >> 1], vf[6][j >> 1], sel));
+                    acc[j] = mfma16<BF16>(va, ph, acc[j]);
+                }
+                if (j > 0) acc[j - 1] = mfma16<BF16>(last, pl, acc[j - 1]);
+                last = va;
             }
             if (more) load_v(kt + kRound, pg);
         }

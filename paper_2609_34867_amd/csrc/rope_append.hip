@@ -32,12 +32,6 @@ namespace {
 
 constexpr int kWaves = 4;               // wavefronts per work-group
 
-template <bool BF16>
-__device__ __forceinline__ v2f unpack2(uint32_t x) {
-    if constexpr (BF16) return v2f{__uint_as_float(x << 16), __uint_as_float(x & 0xFFFF0000u)};
-    else return __builtin_convertvector(__builtin_bit_cast(v2h, x), v2f);
-}
-
 template <bool BF16, int D, bool STREAM>
 __global__ __launch_bounds__(64 * kWaves) void k_rope_append(RopeAppend a) {
     constexpr int kChunks = D / 16;                 // lanes per head: 8 + 8 values each

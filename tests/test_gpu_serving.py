@@ -590,6 +590,27 @@ def test_decode_far_scores(dtype, D, scale, sign, keys):
         assert_within(out[b:b + 1], O, far_bound(O, A, dtype), f"sequence {b}")
 
 
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("Hq,Hk,D", [(4, 4, 128), (16, 1, 128), (24, 2, 64)])
+def test_decode_weights_are_not_rounded_to_16_bits(dtype, Hq, Hk, D):
+    """Flat rows, where one rounding per weight would show: weights in two pieces (the first cut off: eps, the
+    second rounded: eps / 2 of that) are within eps^2 / 2 of themselves (fp16: or m 2^-31 max|v| in all); scores, sums and output as in the module's docstring."""
+    g, lens, P = gen(90), [7, 33, 100, 180], 16
+    kc, vc, table = make_cache(g, dtype, lens, Hk, D, P)
+    q = randn(g, dtype, 4, Hq * D, std=0.05)
+    out = f64(p4q.attention_decode(q, kc, vc, table, ints(lens), Hq)).reshape(-1, Hq, D)
+    tab, k64, v64, q64, eps = table.cpu().numpy(), f64(kc), f64(vc), f64(q).reshape(-1, Hq, D), torch.finfo(DT[dtype]).eps
+    for b, m in enumerate(lens):
+        k, v = (oracle.cache_rows(c, tab[b], m) for c in (k64, v64))
+        O, A = oracle.grouped_attention(q64[b:b + 1], k, v)
+        G, norm = Hq // Hk, np.sqrt((q64[b:b + 1] ** 2).sum(-1))
+        score = 2 * (D * 2.0 ** -24 * norm * np.repeat(np.sqrt((k ** 2).sum(-1)).max(0), G) / np.sqrt(D) + 2.0 ** -22)
+        inner = (eps ** 2 / 2 + score[:, :, None] + 2 * m * 2.0 ** -24) * A
+        if dtype == "fp16":
+            inner = inner + m * 2.0 ** -31 * np.repeat(np.abs(v).max((0, 2)), G)[None, :, None]
+        assert_within(out[b:b + 1], O, inner + eps / 2 * (np.abs(O) + inner) + 2.0 ** -25, f"sequence {b}")
+
+
 def test_offsets_in_the_cache_pass_32_bits():
     """A cache of more than 2^31 elements: append to, attend over and decode from
     its last pages."""
