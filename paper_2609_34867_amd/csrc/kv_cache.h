@@ -32,6 +32,14 @@ constexpr int page_column(int64_t key, int shift, int max_pages) {
     return key >= 0 && (key >> shift) < max_pages ? (int)(key >> shift) : kNoPage;
 }
 
+// the table column that the rows from `key` on are fetched by, in a sequence whose first
+// `keys` keys the table holds: a key past the last one (fetched ahead, never used) goes
+// by the last one's, so that no entry past the sequence's keys is read; kNoPage
+// without keys
+constexpr int fetch_column(int key, int keys, int shift) {
+    return keys > 0 ? (key < keys ? key : keys - 1) >> shift : kNoPage;
+}
+
 // element offset of row `slot` (0 .. P - 1) of head h on `page`, 64 bits: a cache
 // of a few hundred thousand keys passes 2^31 elements
 constexpr int64_t page_row(int page, int Hk, int h, int shift, int slot, int D) {

@@ -173,10 +173,13 @@ __global__ __launch_bounds__(64 * kNW, D == 64 ? 4 : 2) void k_prompt_attention(
     }
     const uint32_t lds0 = lds_addr(smem) + (uint32_t)(wave * NI * 1024);
     const int32_t *table = PAGED ? a.table + (int64_t)t.b * a.max_pages : nullptr;
-    // the page of this wavefront's rows of tile kt (PAGED; a tile past the last: any)
+    // the page of this wavefront's rows of tile kt (PAGED; a tile past the last: the last's)
     auto page_of = [&](int kt) __attribute__((always_inline)) {
         if constexpr (!PAGED) return 0;
-        else return uniform_load(table, min((kt * kKT + 16 * wave) >> a.shift, a.max_pages - 1));
+        else {
+            const int c = fetch_column(kt * kKT + 16 * wave, t.cap, a.shift);
+            return c == kNoPage ? kNoPage : uniform_load(table, c);
+        }
     };
     // (no tile kt: empty descriptors, nothing is read)
     auto issue = [&](bool isv, int kt, int page) __attribute__((always_inline)) {

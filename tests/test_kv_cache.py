@@ -16,6 +16,7 @@ extern "C" {
 int shift_of(int page_size) { return page_shift(page_size); }
 int page_of(int entry, int num_pages) { return valid_page(entry, num_pages); }
 int column(long long key, int shift, int max_pages) { return page_column(key, shift, max_pages); }
+int fetched(int key, int keys, int shift) { return fetch_column(key, keys, shift); }
 long long row(int page, int Hk, int h, int shift, int slot, int D) { return page_row(page, Hk, h, shift, slot, D); }
 int count(int len) { return key_count(len); }
 int first(int b, int e, int n) { return packed_span(b, e, n).first; }
@@ -53,6 +54,18 @@ def test_table_entries(kv, entry, page):
                                      (2 ** 40, -1), (-2 ** 40, -1)])
 def test_columns(kv, key, col):
     assert kv.column(key, 5, 3) == col
+
+
+@pytest.mark.parametrize("keys", [1, 15, 16, 17, 63, 64, 65, 2 ** 30 - 1])
+@pytest.mark.parametrize("shift", [4, 6, 12])
+def test_entries_past_the_keys_are_not_fetched(kv, keys, shift):
+    last = (keys - 1) >> shift
+    for key in [*range(0, 200), keys - 1, keys, keys + 127, 2 ** 30 + 128]:
+        assert kv.fetched(key, keys, shift) == (key >> shift if key < keys else last)
+
+
+def test_nothing_is_fetched_without_keys(kv):
+    assert [kv.fetched(key, 0, 4) for key in (0, 1, 64, 128, HIGH)] == [-1] * 5
 
 
 def test_rows_pass_32_bits(kv):
