@@ -149,3 +149,16 @@ def test_calls_on_another_device_pass_everything_on(monkeypatch):
             # (addresses of the tensors made in each call differ)
             got.append([(n, [x for x in a if not (isinstance(x, int) and x > 1 << 20)]) for n, a in rec.calls])
         assert got[0] == got[1] and len(got[0]) == 1
+
+
+def test_stream_handle_without_torchs_private_call(monkeypatch):
+    """A torch build that lacks it: the current stream object's handle."""
+    import importlib.util
+    from types import SimpleNamespace
+    monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream", raising=False)
+    spec = importlib.util.spec_from_file_location("paper_2609_34867_amd.api_of_such_a_build", api.__file__)
+    other = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(other)
+    asked = []
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda d: asked.append(d) or SimpleNamespace(cuda_stream=77))
+    assert other._stream(torch.device("cuda", 3)) == 77 and asked == [torch.device("cuda", 3)]
