@@ -338,6 +338,14 @@ def _ints(t: Optional[torch.Tensor], name: str, n: int) -> None:
         raise ValueError(f"{name} must be a contiguous int32 tensor of shape ({n},), got {t.dtype} {tuple(t.shape)}")
 
 
+def _fits(**sizes: int) -> None:
+    """Sizes that a caller names are 32-bit integers at the C ABI, where a larger one
+    would lose its upper bits instead of being refused."""
+    for name, n in sizes.items():
+        if not -0x80000000 <= n <= 0x7FFFFFFF:
+            raise ValueError(f"{name} = {n} does not fit 32 bits")
+
+
 def _cache_shape(k_cache: torch.Tensor, v_cache: torch.Tensor, block_table: torch.Tensor, q: torch.Tensor, Hq: int):
     """(pages, Hk, page size, D, B, table width) of a paged cache and its table."""
     if q.dtype not in _CODES:
@@ -495,6 +503,7 @@ def attention_prefill_paged(q: torch.Tensor, k_cache: torch.Tensor, v_cache: tor
 def attention_decode_workspace(B: int, Hq: int, Hk: int, D: int, max_len: int, device) -> torch.Tensor:
     """Workspace for attention_decode().  Its head holds arrival counters that start
     at zero (every call leaves them zero again)."""
+    _fits(B=B, Hq=Hq, Hk=Hk, D=D, max_len=max_len)
     with torch.cuda.device(device):
         n = lib().p4q_attention_decode_workspace_bytes(B, Hq, Hk, D, max_len)
         if n == 0:
@@ -518,14 +527,15 @@ def attention_decode(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
     ldq = _rows_of(q, "q", B, Hq * D, dt)
     _ints(seq_lens, "seq_lens", B)
     ldo = Hq * D if out is None else _rows_of(out, "out", B, Hq * D, dt)
+    if max_len is None:
+        max_len = width * page
+    _fits(max_len=max_len)
     if workspace is not None:
         _check(workspace, "workspace", None, torch.uint8)
     dev = q.device
     if _elsewhere(q, k_cache, v_cache, block_table, seq_lens, out, workspace):
         with torch.cuda.device(dev):
             return attention_decode(q, k_cache, v_cache, block_table, seq_lens, Hq, max_len, out, workspace)
-    if max_len is None:
-        max_len = width * page
     if out is None:
         out = torch.empty((B, Hq * D), dtype=dt, device=dev)
     if workspace is None:

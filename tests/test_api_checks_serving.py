@@ -100,6 +100,15 @@ def test_decode_checks():
     raises("workspace must be", api.attention_decode, *ok, workspace=f16(6))
 
 
+def test_sizes_past_32_bits_are_refused():
+    """They would reach the library without their upper bits: 2^32 + 64 keys as 64."""
+    ok = (f16(2, 256), KC, VC, TABLE, LENS, 4)
+    for n in (2 ** 32 + 64, 2 ** 31, -2 ** 32 + 64):
+        raises("max_len = .* does not fit", api.attention_decode, *ok, max_len=n)
+        raises("max_len = .* does not fit", api.attention_decode_workspace, 2, 4, 2, 64, n, "cuda")
+        raises("B = .* does not fit", api.attention_decode_workspace, n, 4, 2, 64, 64, "cuda")
+
+
 # ------------------------------------------------------------------ another device than the current one
 class Recorder:
     """Stands in for the library: keeps what each call is given."""
