@@ -16,6 +16,7 @@ extern "C" {
 int shift_of(int page_size) { return page_shift(page_size); }
 int page_of(int entry, int num_pages) { return valid_page(entry, num_pages); }
 int column(long long key, int shift, int max_pages) { return page_column(key, shift, max_pages); }
+int by(int n, int G) { const Magic g = magic_of(G); return magic_div(n, g.m, g.shift); }
 int fetched(int key, int keys, int shift) { return fetch_column(key, keys, shift); }
 long long row(int page, int Hk, int h, int shift, int slot, int D) { return page_row(page, Hk, h, shift, slot, D); }
 int count(int len) { return key_count(len); }
@@ -87,3 +88,15 @@ def test_lengths_and_spans(kv):
                 assert (f, l) == (b, e)
             if e <= b:
                 assert f == l
+
+
+def test_division_by_multiplication(kv):
+    """n / G for every group size, around multiples of G over the whole range of n."""
+    for G in range(1, 1025):
+        most = HIGH // G
+        for m in {0, 1, 2, 127, 128, 1 << 20, most // 3, most - 1, most}:
+            for n in {m * G - 1, m * G, m * G + 1, m * G + G - 1}:
+                if 0 <= n <= HIGH:
+                    assert kv.by(n, G) == n // G, (n, G)
+        for n in (1 << 24, (1 << 24) - 1, 1 << 30, HIGH - 1, HIGH):
+            assert kv.by(n, G) == n // G, (n, G)
