@@ -204,6 +204,48 @@ def test_rope_append_nonfinite_values():
     assert row[3] == float("inf") and row[3 + D // 2] == float("inf") and torch.isfinite(row).sum() == D - 2
 
 
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("Hq,Hk,D,lens", [(8, 8, 128, [7001, 1, 0, 6003, 5999]), (16, 8, 64, [9001, 12000, 0, 3, 8999])])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_rope_append_of_more_than_128_mib(dtype, Hq, Hk, D, lens, in_place):
+    """Calls that write more than 128 MiB go past the last-level cache: bit for bit what the same tokens
+    give sequence by sequence in calls that write less, and what attention then reads."""
+    g, P, B, pad = gen(14), 64, len(lens), 9
+    T, past = sum(lens) + pad, [5, 0, 3, 64, 100]
+    totals = [n + m for n, m in zip(lens, past)]
+    kc, vc, table = make_cache(g, dtype, totals, Hk, D, P, fill=0.5)
+    kc2, vc2 = kc.clone(), vc.clone()
+    qkv = randn(g, dtype, T, (Hq + 2 * Hk) * D)
+    cols = (slice(0, Hq * D), slice(Hq * D, (Hq + Hk) * D), slice((Hq + Hk) * D, None))
+    place = torch.randint(0, 100000, (T,), generator=g, device=dev()).to(torch.int32)
+    token = (Hq + 3 * Hk) * D * 2
+    assert T * token > 1 << 27 > max(lens) * token                        # the launcher's threshold
+    # sequence by sequence
+    q_ref, k_ref = torch.full((T, Hq * D), 3.0, dtype=DT[dtype], device=dev()), torch.full((T, Hk * D), 3.0, dtype=DT[dtype], device=dev())
+    at = 0
+    for b, n in enumerate(lens):
+        if n:
+            r = slice(at, at + n)
+            p4q.rope_append(*(qkv[r, c] for c in cols), ints([0, n]), table[b:b + 1], kc2, vc2, Hq, cache_lens=ints(past[b:b + 1]),
+                            positions=place[r], q_out=q_ref[r], k_out=k_ref[r])
+        at += n
+    # in one call
+    wide = qkv.clone()
+    if in_place:
+        q_out, k_out = wide[:, cols[0]], wide[:, cols[1]]
+        q_ref[at:], k_ref[at:] = q_out[at:], k_out[at:]
+    else:
+        gq, gk = Guarded((T, Hq * D), DT[dtype], "q_out"), Guarded((T, Hk * D), DT[dtype], "k_out")
+        q_out, k_out = gq.t.fill_(3), gk.t.fill_(3)
+    p4q.rope_append(*(wide[:, c] for c in cols), cu_of(lens), table, kc, vc, Hq, cache_lens=ints(past), positions=place,
+                    q_out=q_out, k_out=k_out)
+    got = [p4q.attention_decode(q_out[:B], *c, table, ints(totals), Hq, max_len=max(totals)) for c in ((kc, vc), (kc2, vc2))]
+    if not in_place:
+        check_canaries(gq, gk)
+    for a, b in ((q_out, q_ref), (k_out, k_ref), (kc, kc2), (vc, vc2), got, (wide[:, cols[2]], qkv[:, cols[2]])):
+        assert torch.equal(a, b)
+
+
 # ------------------------------------------------------------------ packed prompts
 def packed_case(seed, dtype, Hq, Hk, D, lens, key_lens=None, causal=True, pad=0, std=1.0):
     g = gen(seed)
