@@ -653,6 +653,53 @@ def test_decode_weights_are_not_rounded_to_16_bits(dtype, Hq, Hk, D):
         assert_within(out[b:b + 1], O, inner + eps / 2 * (np.abs(O) + inner) + 2.0 ** -25, f"sequence {b}")
 
 
+@pytest.mark.parametrize("dtype,Hq,Hk,D,P,lens", [
+    ("bf16", 32, 8, 128, 32, [16000, 16, 700, 0, 1, 9000, 33, 2500, 4097, 120, 64, 11000, 5, 300]),    # shares of parts and whole units
+    ("fp16", 64, 8, 128, 256, [40001]),                                                                # one long sequence
+    ("fp16", 24, 1, 64, 64, [70000, 0, 12345, 31]),                                                    # two passes over one key head
+    ("bf16", 40, 40, 128, 16, [1217, 672, 900, 1100])])
+def test_decode_many_long_units(dtype, Hq, Hk, D, P, lens):
+    """More than 16 tiles for every compute unit, in units of more than 16 on the mean, which one work-group
+    per compute unit shares: units in parts over many work-groups, parts and whole units in one, and
+    all of them joined.  Sampled heads against the oracle; nothing around the workspace is written,
+    its counters are zero again, and neither what its other bytes hold nor the run shows."""
+    cus = torch.cuda.get_device_properties(dev()).multi_processor_count
+    heads = Hk * -(-(Hq // Hk) // 16)
+    tiles = sum(2 + -(-n // 32) for n in lens) * heads
+    assert tiles > 16 * cus and tiles > 16 * len(lens) * heads
+    g, B, most = gen(91), len(lens), max(lens)
+    kc, vc, table = make_cache(g, dtype, lens, Hk, D, P)
+    q = randn(g, dtype, B, Hq * D)
+    outs = []
+    for fill in (0, 255):
+        ws = Guarded((p4q.attention_decode_workspace(B, Hq, Hk, D, most, dev()).numel(),), torch.uint8, "workspace")
+        ws.t[:32768], ws.t[32768:] = 0, fill
+        out = Guarded((B, Hq * D), DT[dtype], "out")
+        p4q.attention_decode(q, kc, vc, table, ints(lens), Hq, max_len=most, out=out.t, workspace=ws.t)
+        check_canaries(ws, out)
+        assert not ws.t[:32768].any() and not (ws.t[32768:] == fill).all()      # parts have been there
+        outs.append(out.t)
+    assert torch.equal(*outs)
+    got, q64, G = f64(outs[0]).reshape(B, Hq, D), f64(q).reshape(B, Hq, D), Hq // Hk
+    for b, m in enumerate(lens):
+        pages = table[b, :-(-m // P)].long()
+        for hk in {0, Hk // 2, Hk - 1}:
+            k, v = (f64(c[pages, hk].reshape(-1, 1, D)[:m]) for c in (kc, vc))
+            mine = slice(hk * G, (hk + 1) * G)
+            O, A = oracle.grouped_attention(q64[b:b + 1, mine], k, v)
+            assert_within(got[b:b + 1, mine], O, attention_bound(q64[b:b + 1, mine], k, v, O, A, dtype), f"sequence {b}, key head {hk}")
+    # Every tile once: with q = 0 and value rows that name their tile, O counts them.  Equal weights, sums of
+    # whole numbers, one division, one product and the output's rounding.
+    for b, m in enumerate(lens):
+        at = torch.arange(m, device=dev())
+        vc[table[b, at // P].long(), :, at % P] = torch.eye(D, dtype=DT[dtype], device=dev())[at // 32 % D][:, None]
+    out = f64(p4q.attention_decode(torch.zeros_like(q), kc, vc, table, ints(lens), Hq, max_len=most)).reshape(B, Hq, D)
+    for b, m in enumerate(lens):
+        ref = np.bincount(np.arange(m) // 32 % D, minlength=D) / max(1, m)
+        assert_within(out[b], np.broadcast_to(ref, (Hq, D)), np.broadcast_to((torch.finfo(DT[dtype]).eps / 2 + 2.0 ** -21) * ref, (Hq, D)),
+                      f"sequence {b}, counts")
+
+
 def test_offsets_in_the_cache_pass_32_bits():
     """A cache of more than 2^31 elements: append to, attend over and decode from
     its last pages."""
