@@ -506,6 +506,43 @@ def test_paged_bad_pages_give_nan_where_they_are_seen():
     assert not out[:100].any() and torch.equal(out[100:], ref[100:])
 
 
+@pytest.mark.parametrize("dtype,Hq,Hk,D,P", [("fp16", 8, 8, 128, 64), ("bf16", 8, 2, 64, 16)])
+def test_paged_bad_pages_in_split_keys_give_nan_where_they_are_seen(dtype, Hq, Hk, D, P):
+    """The same where the keys of a row tile are split among work-groups and joined: the bad entry in the
+    first, a middle and the last of them, a length past the table (every split knows), and the call
+    without a workspace."""
+    g, lens, keys = gen(66), [70, 5], [5000, 3000]
+    width = -(-5000 // P)
+    kc, vc, table = make_cache(g, dtype, keys, Hk, D, P, width=width)
+    q = randn(g, dtype, 75, Hq * D)
+    ws = p4q.attention_prompt_workspace(75, 2, Hq, Hk, D, width * P, dev())
+    assert ws is not None
+    ws.fill_(255)
+    none = torch.empty(0, dtype=torch.uint8, device=dev())
+    refs = [p4q.attention_prefill_paged(q, kc, vc, cu_of(lens), table, ints(keys), Hq, workspace=w) for w in (ws, none)]
+    assert not (ws == 255).all() and all(torch.isfinite(r).all() for r in refs)          # split, and joined
+
+    def check(tab, have, first):
+        """Tokens of sequence 0 see keys [0, have[0] - 69 + i); those that see key `first` are NaN."""
+        clean = min(70, max(0, first - (have[0] - 70)))
+        for w, ref in zip((ws, none), refs):
+            out = p4q.attention_prefill_paged(q, kc, vc, cu_of(lens), tab, ints(have), Hq, workspace=w)
+            assert torch.isnan(out[clean:70]).all() and torch.isfinite(out[:clean]).all(), (first, clean)
+            assert torch.equal(out[70:], ref[70:])
+            if have == keys:                                                             # (64 keys: a tile)
+                assert torch.equal(out[:max(0, clean - 64)], ref[:max(0, clean - 64)])
+
+    for key in (0, 63, 64, 2500, 4900, 4950, 4999):
+        for entry in (-1, kc.shape[0], -2 ** 31):
+            bad = table.clone()
+            bad[0, key // P] = entry
+            check(bad, keys, key // P * P)
+    full = table.clone()                                                                 # every page there
+    full[0] = table[0, 0]
+    for m in (width * P + 1, width * P + 40, 2 ** 31 - 1):
+        check(full, [m, 3000], width * P)
+
+
 # ------------------------------------------------------------------ decode
 def decode_case(seed, dtype, Hq, Hk, D, P, key_lens, max_len=None, width=None, std=1.0):
     g = gen(seed)
