@@ -85,6 +85,12 @@ def make_cache(g, dtype, key_lens, Hk, D, P, spare=3, width=None, fill=float("na
     return kc, vc, torch.from_numpy(table).to(dev())
 
 
+def make_cache_flat(g, dtype, B, width, Hk, D, P):
+    """(k_cache, v_cache, table) full of keys, `width` pages for each of B sequences, dealt in any order."""
+    kc, vc = (randn(g, dtype, B * width, Hk, P, D) for _ in range(2))
+    return kc, vc, torch.randperm(B * width, generator=g, device=dev()).to(torch.int32).view(B, width)
+
+
 def check_attention(got, q, keys, lens, Hq, D, dtype, causal=True):
     """got [T, Hq D] against the oracle; keys(b) gives k, v [m, Hk, D] in float64."""
     got, q = f64(got).reshape(-1, Hq, D), f64(q).reshape(-1, Hq, D)
@@ -879,3 +885,57 @@ def test_another_stream():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(got, ref)
+
+
+@pytest.mark.parametrize("B", [1, 70])
+def test_an_idle_batch(B):
+    """No sequence has a token, or a key: padding is left as it was, decode gives zeros."""
+    Hq, Hk, D, P, T = 4, 2, 64, 16, 30
+    g = gen(92)
+    kc, vc, table = make_cache(g, "fp16", [20] * B, Hk, D, P, fill=1.5)
+    kc0, vc0 = kc.clone(), vc.clone()
+    qkv = randn(g, "fp16", T, (Hq + 2 * Hk) * D)
+    q, k, v = qkv[:, :Hq * D], qkv[:, Hq * D:(Hq + Hk) * D], qkv[:, (Hq + Hk) * D:]
+    cu, none = cu_of([0] * B), ints([0] * B)
+    outs = [torch.full((T, n * D), 7.0, dtype=torch.float16, device=dev()) for n in (Hq, Hk, Hq, Hq)]
+    p4q.rope_append(q, k, v, cu, table, kc, vc, Hq, cache_lens=ints([20] * B), q_out=outs[0], k_out=outs[1])
+    p4q.attention_packed(q, k, v, cu, Hq, Hk, D, out=outs[2])
+    p4q.attention_prefill_paged(q, kc, vc, cu, table, ints([20] * B), Hq, out=outs[3])
+    assert all((o == 7).all() for o in outs) and torch.equal(kc, kc0) and torch.equal(vc, vc0)
+    out = p4q.attention_decode(randn(g, "fp16", B, Hq * D), kc, vc, table, none, Hq)
+    assert not out.any()
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+def test_the_largest_group(dtype):
+    """1024 query heads on one key head: packed, over the cache, decode."""
+    packed_case(93, dtype, 1024, 1, 64, [3, 0, 9, 1], pad=1)
+    paged_case(94, dtype, 1024, 1, 64, 16, [2, 1], [40, 300])
+    decode_case(95, dtype, 1024, 1, 64, 16, [77, 0, 300])
+
+
+def test_many_sequences():
+    """Batches of thousands, where a sequence is found many steps into the lists."""
+    B, Hq, Hk, D, P = 5000, 2, 1, 64, 16
+    g = gen(96)
+    lens = [(7 * i) % 4 for i in range(B)]
+    have = [(5 * i) % 40 for i in range(B)]
+    qkv = randn(g, "fp16", sum(lens), (Hq + 2 * Hk) * D)
+    q, k, v = qkv[:, :Hq * D], qkv[:, Hq * D:(Hq + Hk) * D], qkv[:, (Hq + Hk) * D:]
+    kc, vc, table = make_cache_flat(g, "fp16", B, 3, Hk, D, P)
+    q_out, k_out = p4q.rope_append(q, k, v, cu_of(lens), table, kc, vc, Hq, cache_lens=ints(have), k_out=torch.empty(sum(lens), Hk * D, dtype=torch.float16, device=dev()))
+    total = [n + m for n, m in zip(lens, have)]
+    packed = p4q.attention_packed(q_out, k_out, v, cu_of(lens), Hq, Hk, D)
+    paged = p4q.attention_prefill_paged(q_out, kc, vc, cu_of(lens), table, ints(total), Hq)
+    ones = randn(g, "fp16", B, Hq * D)
+    step = p4q.attention_decode(ones, kc, vc, table, ints(total), Hq)
+    ends = np.concatenate([[0], np.cumsum(lens)])
+    k64, v64, kc64, vc64 = f64(k_out).reshape(-1, Hk, D), f64(v).reshape(-1, Hk, D), f64(kc), f64(vc)
+    tab = table.cpu().numpy()
+    for b in [*range(0, B, 97), 63, 64, 65, 4095, 4096, B - 1]:
+        r, n = slice(ends[b], ends[b + 1]), lens[b]
+        cached = [oracle.cache_rows(c, tab[b], total[b]) for c in (kc64, vc64)]
+        assert np.array_equal(cached[0][have[b]:], k64[r]) and np.array_equal(cached[1][have[b]:], v64[r])
+        check_attention(packed[r], q_out[r], lambda _: (k64[r], v64[r]), [n], Hq, D, "fp16")
+        check_attention(paged[r], q_out[r], lambda _: cached, [n], Hq, D, "fp16")
+        check_attention(step[b:b + 1], ones[b:b + 1], lambda _: cached, [1], Hq, D, "fp16")
