@@ -286,15 +286,20 @@ int p4q_attention_prefill(p4q_dtype dt, int B, int L, int H, int D,
  *     over j <= i + m - n (causal = 1: the last token sees the last key)
  *     or every j < m (causal = 0),
  *   out[i, h] = sum_j softmax_j(S) v[j, h / (Hq / Hk)];  zeros without a key.
- * Arithmetic as p4q_attention_prefill.  A non-finite value row may also reach
- * tokens whose mask ends less than 64 keys before it.
+ * Arithmetic as p4q_attention_prefill (the softmax weights rounded once to dt),
+ * for finite scores of any size.  A non-finite value row may also reach tokens
+ * whose mask ends less than 64 keys before it.
  *
  * p4q_attention_prefill_paged: the same with the m = seq_lens[b] keys of the
  * cache (int32 [B]; the call's own tokens included, appended before).
  *
  * p4q_attention_decode: one query row per sequence, over its seq_lens[b] keys
- * (its own included; none: zeros).  max_len, a bound of seq_lens, at most
- * max_pages * page_size, decides how the keys are split among work-groups.
+ * (its own included; none: zeros).  The softmax weights multiply v as sums of two
+ * numbers of dt, within 2^-21 (fp16) or 2^-15 (bf16) of themselves; the rest is fp32.
+ * max_len, a bound of seq_lens, at most max_pages * page_size, bounds how many
+ * work-groups share the keys.  Where a sequence's keys are split follows from
+ * max_len and all seq_lens of the call, so its result may change in the last
+ * bits of fp32 sums with the sequences beside it.
  *
  * Layouts: q [T, ldq] (decode: [B, ldq]), k and v [T (packed: Tk), ldk / ldv],
  *   out [T (B), ld_out], q_out and k_out alike, all of dt; rows may be columns
@@ -302,8 +307,9 @@ int p4q_attention_prefill(p4q_dtype dt, int B, int L, int H, int D,
  * Workspaces: p4q_attention_prompt_workspace_bytes (for both prompt calls;
  *   most_keys bounds the keys of a sequence: Tk, or max_pages * page_size) is
  *   nonzero where few rows meet many keys; given that much (16-byte aligned)
- *   the call splits the keys of a row among work-groups, without it the call
- *   runs unsplit, and the two agree within the rounding of fp32 sums.  Nothing
+ *   the call splits the keys of a row among work-groups, with ws NULL, smaller or
+ *   misaligned it runs unsplit, and the two agree within the rounding of the weights
+ *   and of fp32 sums.  Nothing
  *   of it is read before the call has written it.
  *   p4q_attention_decode_workspace_bytes: required, 16-byte aligned; its first
  *   32768 bytes hold arrival counters, which must be zero before the first

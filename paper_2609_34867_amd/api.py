@@ -411,7 +411,8 @@ def attention_prompt_workspace(T: int, B: int, Hq: int, Hk: int, D: int, most_ke
                                device) -> Optional[torch.Tensor]:
     """Workspace for attention_packed() (most_keys: rows of k) and
     attention_prefill_paged() (most_keys: keys that a row of the table can
-    hold), or None where the call splits nothing.  Its contents do not matter."""
+    hold), or None where the call splits nothing.  Its contents do not matter; a call
+    given a smaller one, or one that is not 16-byte aligned, splits nothing."""
     with torch.cuda.device(device):
         n = lib().p4q_attention_prompt_workspace_bytes(T, B, Hq, Hk, D, most_keys)
         return torch.empty(n, dtype=torch.uint8, device=device) if n else None
@@ -520,8 +521,9 @@ def attention_decode(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
     (p4q_attention_decode): q [B, >= Hq*D], seq_lens int32 [B] (keys of each
     sequence, the new one included; 0: zeros), max_len a bound of them (default:
     what a row of block_table holds).  Without `workspace` the call makes one (and
-    clears its counters); a given one must come from attention_decode_workspace() and
-    serve one call at a time.  Returns out [B, Hq*D]."""
+    clears its counters, a launch more); a given one must come from
+    attention_decode_workspace() and serve one call at a time.  A sequence's result may
+    change in the last bits of fp32 sums with the lengths beside it.  Returns out [B, Hq*D]."""
     pages, Hk, page, D, B, width = _cache_shape(k_cache, v_cache, block_table, q, Hq)
     dt = q.dtype
     ldq = _rows_of(q, "q", B, Hq * D, dt)

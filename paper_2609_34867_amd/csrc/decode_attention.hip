@@ -2,9 +2,10 @@
 //     O[b, h] = sum_{j < len_b} softmax_j(<q_bh, k_j> / sqrt(D)) v_j,
 // with the Hq / Hk query heads of a group reading the same keys.
 //
-// Every key and value is read once and used for a handful of queries, so the call
-// is bound by the bytes of the cache.  A unit of work is (sequence, key head, up to 16
-// query heads of its group); the four wavefronts of a work-group take its tiles of 32
+// Every key and value is used for a handful of queries, so the call is bound by the
+// bytes of the cache.  A unit of work is (sequence, key head, up to 16 query heads of its
+// group): keys and values are read once per 16 query heads on them (24/1 heads twice, 8
+// sequences of 16001 keys 32 us; 16/1 heads once, 27); the four wavefronts of a work-group take its tiles of 32
 // keys in turn, straight from memory to registers, where both products run on
 // v_mfma_f32_16x16x32 with the queries as columns -- with one query 15 columns are
 // idle, but the matrix instructions still take a tenth of the time that the bytes do,
@@ -22,7 +23,7 @@
 //    (one of 131071 keys: 147 us).
 // The softmax keeps a running maximum per query, raised only when a tile exceeds it
 // by more than 2^8 (exp2 units).  The matrix instructions take weights of the cache's
-// type, so each goes in as two such numbers, its rounding and what that left out: within
+// type, so each goes in as two such numbers, the value cut off to one and the rest: within
 // 2^-15 (bf16) and 2^-21 (fp16) of itself, where one alone is off by 2^-8 and 2^-11 and
 // makes the outputs' error 1.3 times what rounding them costs.  Their products run under
 // the loads (64 ragged sequences 132 us, with one piece 129; one of 131071 keys 91.7 either
@@ -34,15 +35,16 @@
 // ends anywhere; a unit's parts, one per work-group, are left in the workspace
 // (device-coherent atomic stores, complete before the work-group counts itself in),
 // and the one that arrives last adds them up, in a fixed order: results do not
-// depend on the order of arrival.  Chunks of the longest length instead: 64 sequences of
-// 16 to 16000 keys 270 us, now 130.
+// depend on the order of arrival.  Where a unit is split follows from all lengths of the call,
+// so its last bits change with its neighbours.  Chunks of the longest length instead: 64
+// sequences of 16 to 16000 keys 270 us, now 130.
 // Rows of the cache past a sequence's length are never used: their scores are
 // masked and their values replaced by zeros.
 //
-// One sequence of 131071 keys, 8 key heads: 91 us (5.9 TB/s; a plain read of as much
-// memory 99 us); the 64 ragged sequences 130 us (5.9 TB/s), 16 sequences of 672 to 1217
-// keys, 32 key heads, 48 us (5.2 TB/s); one of 371 keys, 40 heads, 8.3 us: launch, lengths,
-// table, keys, values and the join in LDS one after the other.
+// One sequence of 131071 keys, 8 key heads: 85 to 92 us (5.8 to 6.3 TB/s; a plain read of as
+// much memory 99 us); the 64 ragged sequences 128 to 132 us (5.8 to 6.0 TB/s), 16 sequences of
+// 672 to 1217 keys, 32 key heads, 44 to 49 us (5.1 to 5.6 TB/s); one of 371 keys, 40 heads, 8.6
+// us: launch, lengths, table, keys, values and the join in LDS one after the other.
 #include "attention_device.h"
 #include "gemm_device.h"
 #include "kv_cache.h"
@@ -58,10 +60,13 @@ constexpr int kWaves = 4;
 constexpr int kKeys = 32;                       // keys of a tile
 constexpr int kRound = kWaves * kKeys;          // keys that a work-group takes at a time
 constexpr int kCols = 16;                       // queries of a work-group
-constexpr int kUnitCost = 2;                    // tiles that a unit's start and end are worth (64 ragged sequences:
-                                                // 133 us, without 156)
-constexpr int kShort = 16;                      // mean tiles of a unit up to which none is split for its own sake
-                                                // (371 keys, 40 heads: whole 8.2 us, in parts 11 to 12)
+constexpr int kUnitCost = 2;                    // tiles that a unit's start and end are worth (us with 1, 2 and 4: 64
+                                                // sequences of 16 to 4000 keys, 32/8 heads, 57, 52, 51; one of 700 keys,
+                                                // 40 heads, 12.8, 9.9, 11.2)
+constexpr int kShort = 16;                      // mean tiles of a unit up to which none is split for its own sake (whole and
+                                                // in parts, us: 200 keys, 40 heads 7.8 and 12.2, 371 keys 10.1 and 11.4,
+                                                // 700 keys 14.7 and 9.9; 4 x 300 to 600 keys, 32/8 heads, 16.2 and 12.2,
+                                                // where it costs most)
 constexpr float kRescale = 8.0f;                // raise the running max past this margin (exp2 units)
 constexpr int kGroupsPerCu = 2;                 // resident work-groups (250 registers)
 constexpr size_t kArrivalBytes = 32768;         // arrival counters at the head of the workspace
@@ -139,10 +144,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_decode_attention(DecodeAtten
         int64_t groups = units, most = gridDim.x;
         if (mean > kShort) {
             // A unit is split into whole rounds of the wavefronts, fewer and longer ones the
-            // more there are to join (1000 keys, 32 heads: 11.5 us, in one part each 22).
+            // more there are to join, and the more queries each part holds (us with half as many
+            // rounds, these, and twice as many: 4000 keys, 24/1 heads 17.3, 14.6, 16.6, 30000 keys
+            // 30.9, 27.1, 33.0, 4000 keys, 32/8 heads 13.6, 13.5, 14.9; without the 2 for many
+            // queries, 24/1 heads, 17.2 and 29.4).
             // With much to read one work-group per CU does best: it has fewer parts to
-            // join (131071 keys: 91 us, with two 101; short units, whose start and end weigh
-            // more, keep two: 64 sequences of 30 to 200 keys 34 us, with one 42).
+            // join (us with one and with two: 131071 keys 91 and 101, 32 x 2000 to 2500 keys, 32/8
+            // heads, 55.5 and 60.1, 8 x 100 to 30000 35.8 and 39.9; below the line, where two are
+            // used, 16000 keys 20.9 and 26.0, 2000 keys 11.8 and 11.8; short units, whose start and
+            // end weigh more, keep two: 64 sequences of 30 to 200 keys 34, with one 42).
             const int rounds = max(1, (int)(__builtin_sqrtf((float)mean * (block > 8 ? 2 : 1)) * 0.125f + 0.5f));
             groups = max(units, div_floor(all, kWaves * rounds));
             if (all > 16 * (int64_t)a.cus) most = min(most, (int64_t)a.cus);

@@ -19,27 +19,40 @@
 //    lies there.  A wavefront fills 16 consecutive rows of a tile, which lie on one
 //    page of a paged cache (16 rows or more), so a page costs a wavefront one table
 //    entry per tile, fetched a tile ahead.
+//  * Weights are rounded to the cache's type before they multiply v, as in the causal prefill
+//    kernel; scores, maxima, sums and accumulators are fp32.  The outputs are then 1.2 to 1.4
+//    times as far from the exact ones as rounding them alone would leave them (fp16 2.5 to
+//    2.9 10^-4 for 2.1, bf16 2.0 to 2.3 10^-3 for 1.6, relative).  Weights in two pieces (as
+//    decode attention has them, which waits for memory meanwhile) need half as many matrix
+//    instructions again: 8191 tokens 700 us for 510, 16 ragged prompts 184 for 146, 10 x
+//    577 at D = 64 46 for 38, 371 tokens 15.6 for 13.6.
 //  * fp16 weights carry 2^7, which moves what they can hold (2^-24) that much further
 //    below the largest.
 // Lengths live on the device: the host launches T G / 128 + B row tiles per key
 // head, which is never too few, and each work-group finds its sequence by a prefix
-// sum over the lengths (64 at a time).
+// sum over the lengths (64 at a time; 1024 sequences of 16 tokens, 32/8 heads, 167 us, 4096
+// of them 1430).  Row tiles are numbered head by head, longest first, and each
+// XCD takes a contiguous eighth of them, so that it reads few heads' keys.  With 8 heads or a
+// multiple all XCDs then have as much to do; with others they do not (one prompt of 8191
+// tokens: up to 1.5 times the mean at 4 heads, 1.8 at 1 or 2, from the mapping).
 //
 // Few rows over many keys do not fill the device.  Then the keys of a row tile are
 // split among work-groups, which leave unnormalized sums in the workspace; a second
 // launch joins them in the order of the splits.
 //
-// One prompt of 8191 tokens, 32/8 heads, bf16: 490 to 527 us from card to card (1.04 to
-// 1.12 PFLOP/s; a large library product reaches 1.40).  Its MFMAs keep the matrix units
-// busy for 54% of the cycles, and the clock is the power limit's: the same call on zeros takes
-// 387 us.  A form that computes the next tile's scores under this tile's softmax needs a
-// fifth fewer cycles and, at the lower clock that it is left, as much time.  16 prompts of
-// 9 to 2003 tokens: 148 us, 25 per work-group, of it 4 before the first tile (lengths, then
-// rows and keys) and 1.8 per tile.  One of 371 tokens, 40 heads: 13.6 us, six tiles one after the
+// One prompt of 8191 tokens, 32/8 heads, bf16: 490 to 530 us from card to card (1.04 to
+// 1.12 PFLOP/s; a large library product reaches 1.40), single passes under the profiler 530 to
+// 620.  Its MFMAs keep the matrix units busy for 55% of the cycles, vector instructions for 51%,
+// and the clock is the power limit's: the same call on zeros takes 387 us.  A form that
+// computes the next tile's scores under this tile's softmax needs a fifth fewer cycles and, at
+// the lower clock that it is left, as much time.  16 prompts of 9 to 2003 tokens: 139 to 146
+// us, 25 per work-group, of it 4 before the first tile (lengths, then
+// rows and keys) and 1.8 per tile.  One of 371 tokens, 40 heads: 12.7 to 13.6 us, six tiles one after the
 // other at 1.3 each.  Not kept, none faster: three tiles in flight; two key halves per row tile
 // in one work-group (371 tokens 14.5 us); sequences in order of length (4 of 300 to 4000
 // tokens, D = 64: 102 for 93 us).  D = 64 runs four wavefronts per SIMD (128 registers, 40
-// sequences of 577 tokens, 20 heads, 110 us; three of them 117).
+// sequences of 577 tokens, 20 heads, 108 us; three of them 117): vector instructions take 71%
+// of the cycles, the matrix units 36%; 10 such sequences (33 to 38 us) 43% and 21%.
 #include "attention_device.h"
 #include "gemm_device.h"
 #include "kv_cache.h"
@@ -58,7 +71,9 @@ constexpr int kQB = kNW * kQW;          // rows per work-group
 constexpr int kKT = 64;                 // keys per tile
 constexpr float kRescale = 8.0f;        // raise the running max past this margin (exp2 units)
 constexpr float kFar = 1024.0f;         // largest maximum (exp2 units) whose rounding costs a weight less than 2^-14
-constexpr int kSplitTiles = 4;          // a split has at least this many tiles (if the row tile has)
+constexpr int kSplitTiles = 4;          // a split has at least this many tiles, if the row tile has (us with 2, 4 and 8 of them:
+                                        // 5 tokens over 4000 keys, 32/8 heads, 21.0, 18.4, 20.4; 60 over 1000
+                                        // 20.5, 18.8, 22.8)
 constexpr int kMaxSplits = 32;
 
 // LDS placement of 16-byte chunk c of row r (D/8 chunks).  K: the rows that a
@@ -484,8 +499,10 @@ int64_t row_tiles(int T, int B, int G) { return (int64_t)T * G / kQB + B; }
 
 // What a split saves is the time of the tiles, about 1.3 us each; what it costs is the
 // join: 33 ns per row tile and split to write and read the sums.  The sum of both
-// is least at sqrt(tiles * gain) splits.  (5 tokens over 20005 keys, 32/8 heads: 32 splits
-// 34 us, 16 of them 36; 1000 tokens: none 25 us, two 35.)
+// is least at sqrt(tiles * gain) splits.  32/8 heads, us with a quarter of this gain, with it,
+// with four times as much, and unsplit: 5 tokens over 20000 keys 33.6, 33.6, 33.5, 324; 60 over 4000
+// 30.9, 31.1, 34.2, 78; 300 over 4000 57, 45, 44, 82; 300 over 1000 29.0, 29.2, 31.9, 30.0; 1000
+// over 1000 earlier ones 46, 55, 46, 47, where it costs most; 1000 over 20000 340, 338, 336, 383.
 float split_gain(int T, int Hq) { return 40.0f * kQB / ((float)T * (float)Hq); }
 
 // work-groups that share the keys of a row tile, at most

@@ -16,8 +16,8 @@
 // reads its 8 sines and cosines once and keeps them in registers.  A step of a
 // wavefront covers 1024 / D heads with two 16-byte loads and stores per lane.
 // Products and sums are fp32 (one fma), each result rounded once to 16 bits.
-// What bounds it: bytes for prompts (16 of 656 to 704 tokens, 32 heads: 120 us, 5.2 TB/s,
-// a plain copy reaches 4.7), the chain of dependent loads (lengths, table, page) for a
+// What bounds it: bytes for prompts (16 of 656 to 704 tokens, 32 heads, 10927 in all: 120 us,
+// 5.2 TB/s, a plain copy reaches 4.7), the chain of dependent loads (lengths, table, page) for a
 // decode step (3.3 us of kernel).
 #include "attention_device.h"
 #include "gemm_device.h"
@@ -136,9 +136,14 @@ hipError_t launch_rope_append(p4q_dtype dt, int D, RopeAppend a, float rope_base
         return hipGetLastError();
     };
     // More than the last-level cache (256 MB) can hand on to the attention that follows
-    // is written past it.  16 prompts of 704 tokens, 32 heads (313 MB written): 120 us, 130
-    // through the cache, and with the attention 240 and 242; one prompt (20 MB): 12.4 us and
-    // 12.0, with the attention 31.8 and 29.7.
+    // is written past it.  Prompts of 704 tokens, 32 heads, with k_out, us past the cache and
+    // through it, alone and (in brackets) with attention_packed behind:
+    //   D = 128: 1 (23 MB written) 10.9, 10.1 (31.0, 28.0); 4 (92 MB) 32, 37 (72, 71); 8 (185 MB)
+    //   63, 71 (131, 131); 16 (369 MB) 123, 131 (249, 244); 32 (738 MB) 244, 254 (478, 473)
+    //   D = 64: 4 (46 MB) 18.4, 15.9 (47.4, 43.9); 8 (92 MB) 34, 45 (81, 81); 16 (185 MB) 72, 78
+    //   (142, 143); 32 (369 MB) 137, 146 (266, 269)
+    // Above the line the append alone is 4 to 11% faster past the cache and both calls are
+    // within 2% either way; far below it the attention then pays for the reads.
     const bool stream_out = (int64_t)a.T * (a.Hq + (a.k_out ? 3 : 2) * a.Hk) * D * 2 > (int64_t)128 << 20;
     auto d = [&](auto bf, auto st) {
         return D == 128 ? go(k_rope_append<decltype(bf)::value, 128, decltype(st)::value>)
