@@ -34,7 +34,7 @@
 // of them 1430).  Row tiles are numbered head by head, longest first, and each
 // XCD takes a contiguous eighth of them, so that it reads few heads' keys.  With 8 heads or a
 // multiple all XCDs then have as much to do; with others they do not (one prompt of 8191
-// tokens: up to 1.5 times the mean at 4 heads, 1.8 at 1 or 2, from the mapping).
+// tokens: up to 1.5 times the mean at 4 heads, 1.7 at 2, 1.9 at 1, from the mapping).
 //
 // Few rows over many keys do not fill the device.  Then the keys of a row tile are
 // split among work-groups, which leave unnormalized sums in the workspace; a second
