@@ -295,7 +295,7 @@ int p4q_attention_prefill(p4q_dtype dt, int B, int L, int H, int D,
  *
  * p4q_attention_decode: one query row per sequence, over its seq_lens[b] keys
  * (its own included; none: zeros).  The softmax weights multiply v as sums of two
- * numbers of dt, within 2^-21 (fp16) or 2^-15 (bf16) of themselves; the rest is fp32.
+ * numbers of dt, within 2^-20 (fp16) or 2^-14 (bf16) of themselves; the rest is fp32.
  * max_len, a bound of seq_lens, at most max_pages * page_size, bounds how many
  * work-groups share the keys.  Where a sequence's keys are split follows from
  * max_len and all seq_lens of the call, so its result may change in the last

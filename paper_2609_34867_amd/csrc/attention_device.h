@@ -14,6 +14,7 @@ typedef _Float16 v2h __attribute__((ext_vector_type(2)));
 typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
 typedef float v2f __attribute__((ext_vector_type(2)));
 typedef int v2i __attribute__((ext_vector_type(2)));
+typedef unsigned short v2u __attribute__((ext_vector_type(2)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 typedef short v4s __attribute__((ext_vector_type(4)));
@@ -42,14 +43,16 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     else return __builtin_bit_cast(uint32_t, __builtin_convertvector(v2f{lo, hi}, v2h));
 }
 
-// the same towards zero, of values that are not negative
+// two fp32 >= 0 -> the 16-bit values one step below what cutting them off gives (0: 0)
 template <bool BF16>
-__device__ __forceinline__ uint32_t pack2_down(float lo, float hi) {
-    if constexpr (BF16) return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
-    else return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(lo, hi));
+__device__ __forceinline__ uint32_t pack2_below(float lo, float hi) {
+    uint32_t cut;
+    if constexpr (BF16) cut = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
+    else cut = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(lo, hi));
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_sub_sat(__builtin_bit_cast(v2u, cut), v2u{1, 1}));
 }
 
-// and back
+// 16-bit values -> fp32
 template <bool BF16>
 __device__ __forceinline__ v2f unpack2(uint32_t x) {
     if constexpr (BF16) return v2f{__uint_as_float(x << 16), __uint_as_float(x & 0xFFFF0000u)};

@@ -5,11 +5,11 @@
 // Every key and value is used for a handful of queries, so the call is bound by the
 // bytes of the cache.  A unit of work is (sequence, key head, up to 16 query heads of its
 // group): keys and values are read once per 16 query heads on them (24/1 heads twice, 8
-// sequences of 16001 keys 32 us; 16/1 heads once, 27); the four wavefronts of a work-group take its tiles of 32
-// keys in turn, straight from memory to registers, where both products run on
-// v_mfma_f32_16x16x32 with the queries as columns -- with one query 15 columns are
-// idle, but the matrix instructions still take a tenth of the time that the bytes do,
-// and no key or value is converted or reduced across lanes:
+// sequences of 16001 keys 32 us; 16/1 heads once, 27); the four wavefronts of a
+// work-group take its tiles of 32 keys in turn, straight from memory to registers, where
+// both products run on v_mfma_f32_16x16x32 with the queries as columns -- with one query
+// 15 columns are idle, but the matrix instructions still take a small part of the time that
+// the bytes do, and no key or value is converted or reduced across lanes:
 //  * S^T = K Q^T: row m of matrix tile t is key 8 (m / 4) + 4 t + m % 4 of the 32.
 //    Lane l (m = l % 16, g = l / 16) loads 16-byte pieces 4 s + g of its key.
 //  * The result then has, in lane l, query l % 16 and keys 8 g + 4 t + r: exactly
@@ -23,8 +23,8 @@
 //    (one of 131071 keys: 147 us).
 // The softmax keeps a running maximum per query, raised only when a tile exceeds it
 // by more than 2^8 (exp2 units).  The matrix instructions take weights of the cache's
-// type, so each goes in as two such numbers, the value cut off to one and the rest: within
-// 2^-15 (bf16) and 2^-21 (fp16) of itself, where one alone is off by 2^-8 and 2^-11 and
+// type, so each goes in as two such numbers, one from below and the rest: within
+// 2^-14 (bf16) and 2^-20 (fp16) of itself, where one alone is off by 2^-8 and 2^-11 and
 // makes the outputs' error 1.3 times what rounding them costs.  Their products run under
 // the loads (64 ragged sequences 132 us, with one piece 129; one of 131071 keys 91.7 either
 // way).  fp16 weights carry 2^7, so that they reach down to 2^-31 of the
@@ -117,7 +117,6 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_decode_attention(DecodeAtten
     constexpr int kBatch = 512 / D;             // parts per wavefront of the join at a time
     constexpr int kCoherent = 16;               // sc1: past the caches that other XCDs do not see
     constexpr float kBias = BF16 ? 0.0f : 7.0f;
-    constexpr float kLeast = BF16 ? 0x1p-100f : 0x1p-24f;   // (a weight of 0 becomes this: 2^-31 of the largest)
     __shared__ __attribute__((aligned(16))) float s_acc[kWaves][kCols * kRow];
     __shared__ float s_max[kWaves][kCols], s_sum[kWaves][kCols];
     __shared__ int s_last;
@@ -304,14 +303,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_decode_attention(DecodeAtten
                 w[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[i >> 2][i & 3] - off, a.c2, kBias));
                 sum += w[i];
             }
-            // Each weight as a sum of two 16-bit numbers: the first cut off, not rounded, and
-            // the second never 0, so that neither turns an infinite value into NaN.
+            // Each weight as a sum of two 16-bit numbers.  The first is a step below the cut-off
+            // weight, so that the second is neither 0 nor negative, which would turn an infinite
+            // value into NaN; a weight of 0 stays 0.
             uint32_t hi[4], lo[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                hi[i] = pack2_down<BF16>(w[2 * i], w[2 * i + 1]);
+                hi[i] = pack2_below<BF16>(w[2 * i], w[2 * i + 1]);
                 const v2f h = unpack2<BF16>(hi[i]);
-                lo[i] = pack2<BF16>(__builtin_fmaxf(w[2 * i] - h[0], kLeast), __builtin_fmaxf(w[2 * i + 1] - h[1], kLeast));
+                lo[i] = pack2<BF16>(w[2 * i] - h[0], w[2 * i + 1] - h[1]);
             }
             const uint4 ph = make_uint4(hi[0], hi[1], hi[2], hi[3]), pl = make_uint4(lo[0], lo[1], lo[2], lo[3]);
             // (the second pieces one step behind the first, whose sums they wait for)

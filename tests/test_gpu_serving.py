@@ -678,8 +678,8 @@ def test_decode_far_scores(dtype, D, scale, sign, keys):
 @pytest.mark.parametrize("dtype", ["fp16", "bf16"])
 @pytest.mark.parametrize("Hq,Hk,D", [(4, 4, 128), (16, 1, 128), (24, 2, 64)])
 def test_decode_weights_are_not_rounded_to_16_bits(dtype, Hq, Hk, D):
-    """Flat rows, where one rounding per weight would show: weights in two pieces (the first cut off: eps, the
-    second rounded: eps / 2 of that) are within eps^2 / 2 of themselves (fp16: or m 2^-31 max|v| in all); scores, sums and output as in the module's docstring."""
+    """Flat rows, where one rounding per weight would show: weights in two pieces (the first within 2 eps
+    below, the second rounded: eps / 2 of that) are within eps^2 of themselves (fp16: or m 2^-32 max|v| in all); scores, sums and output as in the module's docstring."""
     g, lens, P = gen(90), [7, 33, 100, 180], 16
     kc, vc, table = make_cache(g, dtype, lens, Hk, D, P)
     q = randn(g, dtype, 4, Hq * D, std=0.05)
@@ -690,10 +690,25 @@ def test_decode_weights_are_not_rounded_to_16_bits(dtype, Hq, Hk, D):
         O, A = oracle.grouped_attention(q64[b:b + 1], k, v)
         G, norm = Hq // Hk, np.sqrt((q64[b:b + 1] ** 2).sum(-1))
         score = 2 * (D * 2.0 ** -24 * norm * np.repeat(np.sqrt((k ** 2).sum(-1)).max(0), G) / np.sqrt(D) + 2.0 ** -22)
-        inner = (eps ** 2 / 2 + score[:, :, None] + 2 * m * 2.0 ** -24) * A
+        inner = (eps ** 2 + score[:, :, None] + 2 * m * 2.0 ** -24) * A
         if dtype == "fp16":
-            inner = inner + m * 2.0 ** -31 * np.repeat(np.abs(v).max((0, 2)), G)[None, :, None]
+            inner = inner + m * 2.0 ** -32 * np.repeat(np.abs(v).max((0, 2)), G)[None, :, None]
         assert_within(out[b:b + 1], O, inner + eps / 2 * (np.abs(O) + inner) + 2.0 ** -25, f"sequence {b}")
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+def test_decode_keys_without_weight_add_nothing(dtype):
+    """One key 10^3 and more above all others in units of log 2, whose weights are 0 in fp32: its value row,
+    here zeros, is the result, however many others there are."""
+    Hq, Hk, D, P, n = 2, 1, 64, 4096, 300000
+    pages = -(-n // P)
+    kc = torch.ones(pages, Hk, P, D, dtype=DT[dtype], device=dev())
+    vc, table = torch.full_like(kc, 9.0), torch.arange(pages, device=dev(), dtype=torch.int32).view(1, -1)
+    q = torch.full((1, Hq * D), 64.0, dtype=DT[dtype], device=dev())        # scores 512, and four times as much
+    for at in (0, 12345, n - 1):
+        k, v = kc.clone(), vc.clone()
+        k[at // P, :, at % P], v[at // P, :, at % P] = 4.0, 0.0
+        assert not p4q.attention_decode(q, k, v, table, ints([n]), Hq).any()
 
 
 @pytest.mark.parametrize("dtype,Hq,Hk,D,P,lens", [
