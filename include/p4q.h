@@ -514,6 +514,97 @@ int p4q_w4a4_linear(int M, int N_out, int K_in,
                     void *ws, size_t ws_bytes, hipStream_t stream);
 
 /* ------------------------------------------------------------------------
+ * W4A4 in microscaled floating point (MXFP4 of the OCP Microscaling
+ * specification 1.0), the 4-bit format that gfx950's matrix instructions
+ * multiply directly: beside the int4 path above, with a scale per 32 values
+ * instead of one per token or output channel.
+ *
+ * The format.  Rows of K values, K % 32 == 0, in blocks of 32 consecutive k:
+ *   X = 2^(floor(log2 max_k |x_k|) - 2), at least 2^-127,
+ *   code_k = the E2M1 number (0, 0.5, 1, 1.5, 2, 3, 4, 6 with a sign) nearest
+ *            to x_k / X, ties to the even code, magnitudes above 6 to 6.
+ *   A code is 4 bits: sign, two bits of exponent, one of mantissa.  Codes
+ *   uint8 [rows, K/2], the even k in the low nibble.  Scales uint8
+ *   [rows, p4q_mx4_scale_stride(K)]: byte b of a row is log2 X + 127 of block
+ *   b; the bytes behind K/32 are padding, which calls write as 0 and whose
+ *   contents no call depends on.  A block with an infinity or a NaN has
+ *   byte 255 and codes 0 and stands for NaNs; a block of zeros has byte 0.
+ *
+ * p4q_mx4_scale_stride: bytes of a row of scales, 16 ceil(K / 512); 0 for K
+ *   outside the limits.
+ *
+ * p4q_quant_mx4: codes and scales of x's rows; unless it is NULL, values
+ *   [M, ldv] (dt) receives what they stand for, exactly (the fake-quantized
+ *   rows).  The same call quantizes weight rows.
+ *
+ * p4q_mx4_linear: y[m][n] = round(sum_k A[m][k] W[n][k]) on the numbers that
+ *   the codes and scales stand for, fp32 sums in an unspecified order, rounded
+ *   once to out_dt.  A NaN block makes a NaN of every output it enters.
+ *
+ * p4q_mx4_gated_linear: w holds 2 N_out rows, the gate's, then the up
+ *   projection's:  g = A W_gate^T, u = A W_up^T in fp32 as above,
+ *   y[m][n] = round(g[m][n] / (1 + exp(-g[m][n])) * u[m][n]).
+ * p4q_mx4_gated_linear_quant: the same, whose result leaves in MXFP4 instead
+ *   (the codes of the fp32 products), ready for the next p4q_mx4_linear;
+ *   N_out % 32 == 0.
+ *
+ * p4q_residual_rmsnorm_quant: what lies between two blocks of a decoder layer.
+ *   r' = post_gamma ? r / rms(r) * post_gamma : r    (the block's output)
+ *   h  = round(fl32(x + alpha * gate * r'))           (gate NULL: 1)
+ *   P4Q_NORM_INT4: (codes, scales) = those of p4q_rmsnorm_quant(h, gamma, eps,
+ *     clip): codes [M, d/2] of Q4, scales fp32 [M];
+ *   P4Q_NORM_MX4: (codes, scales) = MXFP4 of fl32(h * gamma / rms(h)),
+ *   rms(z) = sqrt(sum z^2 / d + eps); a row with sum z^2 / d + eps = 0 counts as
+ *   zeros.  Everything before a stated rounding is held in 64 bits.  h_out
+ *   [M, ldh] (dt) receives h.  With r NULL, h = x, and h_out, gate and
+ *   post_gamma must be NULL, alpha 1.  values, unless NULL: what the codes
+ *   stand for, rounded to dt.  h_out may be x or r (same pointer and row
+ *   stride); other overlaps are not allowed.  gamma, post_gamma and gate are
+ *   [d] of dt.
+ *
+ * Results do not depend on anything but a row's own values (and, of products,
+ *   on M and the sizes through the order of the fp32 sums).  No workspace.
+ * Limits: M >= 1; 32 <= K <= 131072 (products, quantizer), d <= 16384;
+ *   quantizer: M ceil(K / 512) < 2^26; norm: M < 2^23; products: M <= 2^20,
+ *   1 <= N_out <= 2^22; row strides of 16-bit operands >= the row, of x, r,
+ *   h_out and values multiples of 8; ldy >= N_out; eps in [0, 1], alpha finite,
+ *   clip in [2^-16, 1] (P4Q_NORM_MX4: 1); x, r, h_out, values, gamma,
+ *   post_gamma, gate, codes and scales 16-byte aligned (the scales of
+ *   P4Q_NORM_INT4 and y 4-byte).
+ * ---------------------------------------------------------------------- */
+typedef enum p4q_norm_format {
+    P4Q_NORM_INT4 = 0,
+    P4Q_NORM_MX4 = 1,
+    /* not formats: see p4q_dtype */
+    P4Q_NORM_RANGE_MIN_ = -0x7FFFFFFF - 1,
+    P4Q_NORM_RANGE_MAX_ = 0x7FFFFFFF
+} p4q_norm_format;
+
+size_t p4q_mx4_scale_stride(int K);
+
+int p4q_quant_mx4(p4q_dtype dt, int M, int K, const void *x, int64_t ldx, uint8_t *codes,
+                  uint8_t *scales, void *values, int64_t ldv, hipStream_t stream);
+
+int p4q_mx4_linear(int M, int N_out, int K, const uint8_t *a_codes, const uint8_t *a_scales,
+                   const uint8_t *w_codes, const uint8_t *w_scales, p4q_dtype out_dt, void *y,
+                   int64_t ldy, hipStream_t stream);
+
+int p4q_mx4_gated_linear(int M, int N_out, int K, const uint8_t *a_codes, const uint8_t *a_scales,
+                         const uint8_t *w_codes, const uint8_t *w_scales, p4q_dtype out_dt, void *y,
+                         int64_t ldy, hipStream_t stream);
+
+int p4q_mx4_gated_linear_quant(int M, int N_out, int K, const uint8_t *a_codes,
+                               const uint8_t *a_scales, const uint8_t *w_codes,
+                               const uint8_t *w_scales, uint8_t *codes, uint8_t *scales,
+                               hipStream_t stream);
+
+int p4q_residual_rmsnorm_quant(p4q_dtype dt, p4q_norm_format fmt, int M, int d, const void *x,
+                               int64_t ldx, const void *r, int64_t ldr, const void *post_gamma,
+                               const void *gate, float alpha, const void *gamma, float eps,
+                               float clip, void *h_out, int64_t ldh, uint8_t *codes, void *scales,
+                               void *values, int64_t ldv, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
  * Diagnostics: microbenchmarks of the device's own ceilings, against which
  * the kernels above are reported beside the published peaks.  They are not
  * part of the method.

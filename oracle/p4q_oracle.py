@@ -1000,3 +1000,83 @@ def calib_block(x: np.ndarray, weights: dict, gamma1: np.ndarray, gamma2: np.nda
     res["grad_clip_a"] = {g: grads[g][1] for g in BLOCK_GROUPS}
     res["grad_clip_w"] = {g: grads[g][2] for g in BLOCK_GROUPS}
     return res
+
+
+# --------------------------------------------------------------------------
+# O9: W4A4 in microscaled floating point (MXFP4 of the OCP Microscaling
+#     specification 1.0): blocks of 32 values sharing a power of two, elements
+#     E2M1
+# --------------------------------------------------------------------------
+E2M1 = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
+
+
+def mx4_scale_stride(K: int) -> int:
+    """Bytes of a row of scales: one per block, padded to a multiple of 16."""
+    return -(-(K // 32) // 16) * 16
+
+
+def quant_mx4(x: np.ndarray) -> Tuple[np.ndarray, np.ndarray]:
+    """(codes uint8 [M, K/2], scales uint8 [M, mx4_scale_stride(K)]) of rows x of
+    real numbers (float64 holding the operand exactly).
+
+    X = 2^max(floor(log2 max|x|) - 2, -127) per block of 32; the code is the E2M1
+    number nearest to x / X (a border belongs to the neighbour whose code is even),
+    6 for more; a block with a non-finite value has byte 255 and codes 0, one of
+    zeros byte 0."""
+    x = np.asarray(x, dtype=np.float64)
+    M, K = x.shape
+    b = x.reshape(M, K // 32, 32)
+    finite = np.isfinite(b).all(axis=2)
+    b = np.where(finite[:, :, None], b, 0.0)
+    top = np.abs(b).max(axis=2)
+    e = np.where(top > 0, np.frexp(top)[1] - 1 - 2, -127)
+    e = np.maximum(e, -127)
+    z = np.ldexp(b, -e[:, :, None])
+    m = np.abs(z)
+    k = np.zeros(b.shape, dtype=np.uint8)
+    for i in range(7):
+        border = (E2M1[i] + E2M1[i + 1]) / 2
+        k += ((m > border) | ((m == border) & (i % 2 == 1))).astype(np.uint8)
+    code = np.where(finite[:, :, None], k | (np.signbit(z).astype(np.uint8) << 3), 0).reshape(M, K).astype(np.uint8)
+    scales = np.zeros((M, mx4_scale_stride(K)), dtype=np.uint8)
+    scales[:, :K // 32] = np.where(finite, e + 127, 255)
+    return code[:, 0::2] | (code[:, 1::2] << 4), scales
+
+
+def mx4_values(codes: np.ndarray, scales: np.ndarray) -> np.ndarray:
+    """The numbers [M, K] that codes and scales stand for, exactly, in float64."""
+    codes = np.asarray(codes)
+    nib = np.stack([codes & 15, codes >> 4], axis=-1).reshape(codes.shape[0], -1)
+    v = E2M1[nib & 7] * np.where(nib & 8, -1.0, 1.0)
+    byte = np.repeat(scales[:, :v.shape[1] // 32].astype(np.int64), 32, axis=1)
+    return np.where(byte == 255, np.nan, np.ldexp(v, byte - 127))
+
+
+def mx4_linear(a_codes, a_scales, w_codes, w_scales) -> Tuple[np.ndarray, np.ndarray]:
+    """(y, magnitudes): A W^T and |A| |W|^T in float64."""
+    a, w = mx4_values(a_codes, a_scales), mx4_values(w_codes, w_scales)
+    return a @ w.T, np.abs(a) @ np.abs(w).T
+
+
+def residual_rmsnorm(x, gamma, r=None, eps: float = 1e-5, dtype: str = "fp16", post_gamma=None, gate=None,
+                     alpha: float = 1.0) -> Tuple[np.ndarray, np.ndarray]:
+    """(h, n): h = round16(fl32(x + alpha gate r')) in storage dtype, r' = r or, with
+    post_gamma, RMSNorm(r) * post_gamma; n = fl32(RMSNorm(h) * gamma), a row whose mean
+    square + eps is 0 being zeros.  Before a rounding everything is float64."""
+    f64 = lambda t: as_f32(t, dtype).astype(np.float64)  # noqa: E731
+    eps = float(np.float32(eps))
+
+    def inverse(z):
+        ms = np.mean(z * z, axis=1, keepdims=True) + eps
+        return np.where(ms > 0, 1.0 / np.sqrt(np.where(ms > 0, ms, 1.0)), 0.0)
+
+    h = x
+    if r is not None:
+        b = f64(r)
+        if post_gamma is not None:
+            b = b * inverse(b) * f64(post_gamma)
+        if gate is not None:
+            b = b * f64(gate)
+        h = round_out((f64(x) + float(np.float32(alpha)) * b).astype(np.float32), dtype)
+    hw = f64(h)
+    return h, (hw * f64(gamma) * inverse(hw)).astype(np.float32)

@@ -16,6 +16,7 @@ LIB_PATH = os.environ.get("P4Q_LIBRARY") or os.path.join(
 
 P4Q_OK, P4Q_ERR_INVALID_ARG, P4Q_ERR_UNSUPPORTED, P4Q_ERR_WORKSPACE, P4Q_ERR_HIP = range(5)
 P4Q_FP16, P4Q_BF16 = 0, 1
+P4Q_NORM_INT4, P4Q_NORM_MX4 = 0, 1
 
 _c_int, _c_size, _c_i64, _c_float, _vp = (ctypes.c_int, ctypes.c_size_t, ctypes.c_int64,
                                           ctypes.c_float, ctypes.c_void_p)
@@ -69,6 +70,14 @@ SIGNATURES = {
     "p4q_w4a4_linear_workspace_bytes": (_c_size, [_c_int, _c_int, _c_int]),
     "p4q_w4a4_linear": (_c_int, [_c_int, _c_int, _c_int, _vp, _vp, _vp, _vp, _c_int, _vp,
                                  _c_i64, _vp, _vp, _c_size, _vp]),
+    "p4q_mx4_scale_stride": (_c_size, [_c_int]),
+    "p4q_quant_mx4": (_c_int, [_c_int, _c_int, _c_int, _vp, _c_i64, _vp, _vp, _vp, _c_i64, _vp]),
+    "p4q_mx4_linear": (_c_int, [_c_int, _c_int, _c_int, _vp, _vp, _vp, _vp, _c_int, _vp, _c_i64, _vp]),
+    "p4q_mx4_gated_linear": (_c_int, [_c_int, _c_int, _c_int, _vp, _vp, _vp, _vp, _c_int, _vp, _c_i64, _vp]),
+    "p4q_mx4_gated_linear_quant": (_c_int, [_c_int, _c_int, _c_int, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "p4q_residual_rmsnorm_quant": (_c_int, [_c_int, _c_int, _c_int, _c_int, _vp, _c_i64, _vp, _c_i64, _vp, _vp,
+                                            _c_float, _vp, _c_float, _c_float, _vp, _c_i64, _vp, _vp, _vp, _c_i64,
+                                            _vp]),
     "p4q_diag_mfma_i8": (_c_int, [_c_int, _c_int, _vp, _vp]),
     "p4q_diag_stream_read": (_c_int, [_vp, _c_size, _c_int, _vp, _vp]),
 }

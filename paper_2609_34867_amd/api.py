@@ -11,7 +11,8 @@ from typing import Optional, Tuple
 
 import torch
 
-from ._lib import P4Q_BF16, P4Q_ERR_INVALID_ARG, P4Q_FP16, P4QError, check, lib
+from ._lib import (P4Q_BF16, P4Q_ERR_INVALID_ARG, P4Q_FP16, P4Q_NORM_INT4, P4Q_NORM_MX4, P4QError, check,
+                   lib)
 
 
 def version() -> str:
@@ -761,6 +762,178 @@ def w4a4_linear(a_codes: torch.Tensor, a_scales: torch.Tensor, w_codes: torch.Te
                                _ptr(acc_out), _ptr(workspace), ws_bytes, _stream(dev))
     check(st)
     return (y, acc_out) if return_acc else y
+
+
+# --------------------------------------------------------------------------- MXFP4
+def mx4_scale_stride(K: int) -> int:
+    """Bytes of a row of MXFP4 scales (p4q_mx4_scale_stride): one per 32 values,
+    padded to a multiple of 16."""
+    return (K + 511) // 512 * 16
+
+
+def _mx4_rows(codes: torch.Tensor, scales: torch.Tensor, name: str) -> Tuple[int, int]:
+    """(rows, K) of an MXFP4 operand."""
+    if codes.dim() != 2 or codes.dtype is not torch.uint8 or not codes.is_contiguous():
+        raise ValueError(f"{name}_codes must be a contiguous uint8 [rows, K/2] tensor, got {codes.dtype} {tuple(codes.shape)}")
+    rows, K = codes.shape[0], 2 * codes.shape[1]
+    want = (rows, mx4_scale_stride(K))
+    if scales.shape != want or scales.dtype is not torch.uint8 or not scales.is_contiguous():
+        raise ValueError(f"{name}_scales must be a contiguous uint8 tensor of shape {want}, got {scales.dtype} {tuple(scales.shape)}")
+    return rows, K
+
+
+def _mx4_out(codes, scales, rows: int, K: int, dev):
+    """The given buffers of an MXFP4 result, checked, or new ones."""
+    _check(codes, "codes", (rows, K // 2), torch.uint8)
+    _check(scales, "scales", (rows, mx4_scale_stride(K)), torch.uint8)
+    if codes is None:
+        codes = torch.empty((rows, K // 2), dtype=torch.uint8, device=dev)
+    if scales is None:
+        scales = torch.empty((rows, mx4_scale_stride(K)), dtype=torch.uint8, device=dev)
+    return codes, scales
+
+
+def quant_mx4(x: torch.Tensor, codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
+              values: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """MXFP4 quantization of rows (p4q_quant_mx4): x [M, K] (row stride may exceed
+    K) -> (codes uint8 [M, K/2], scales uint8 [M, mx4_scale_stride(K)]), one power
+    of two per 32 values.  `values` [M, K] of x's dtype, if given, receives the
+    numbers that they stand for (the fake-quantized rows)."""
+    if x.dim() != 2:
+        raise ValueError("x must be 2-D")
+    M, K = x.shape
+    ldx = _rows_of(x, "x", M, K, x.dtype if x.dtype in _CODES else torch.float16)
+    ldv = 0 if values is None else _rows_of(values, "values", M, K, x.dtype)
+    _check(codes, "codes", (M, K // 2), torch.uint8)
+    _check(scales, "scales", (M, mx4_scale_stride(K)), torch.uint8)
+    dev = x.device
+    if _elsewhere(x, codes, scales, values):
+        with torch.cuda.device(dev):
+            return quant_mx4(x, codes, scales, values)
+    codes, scales = _mx4_out(codes, scales, M, K, dev)
+    check(lib().p4q_quant_mx4(_CODES[x.dtype], M, K, x.data_ptr(), ldx, codes.data_ptr(), scales.data_ptr(),
+                              _ptr(values), ldv, _stream(dev)))
+    return codes, scales
+
+
+def residual_rmsnorm_quant(x: torch.Tensor, gamma: torch.Tensor, r: Optional[torch.Tensor] = None, eps: float = 1e-5,
+                           fmt: str = "mx4", clip: float = 1.0, post_gamma: Optional[torch.Tensor] = None,
+                           gate: Optional[torch.Tensor] = None, alpha: float = 1.0,
+                           h_out: Optional[torch.Tensor] = None, codes: Optional[torch.Tensor] = None,
+                           scales: Optional[torch.Tensor] = None, values: Optional[torch.Tensor] = None):
+    """A block's output added to the residual, and the next block's RMSNorm of the
+    sum, quantized (p4q_residual_rmsnorm_quant): h = x + alpha * gate * r (r first
+    normalized and scaled by post_gamma where that is given), then RMSNorm(h) * gamma
+    as MXFP4 (fmt "mx4": scales uint8 [M, mx4_scale_stride(d)]) or int4 per token
+    (fmt "int4", with clip, as rmsnorm_quant(): scales fp32 [M]).
+
+    x, r [M, d] (row strides may exceed d); gamma, post_gamma and gate [d] of x's dtype.
+    Returns (codes, scales, h); without r, h is x.  h_out may be x or r; `values`
+    [M, d], if given, receives what the codes stand for, rounded to x's dtype."""
+    if x.dim() != 2:
+        raise ValueError("x must be 2-D")
+    if fmt not in ("mx4", "int4"):
+        raise ValueError(f"fmt must be 'mx4' or 'int4', got {fmt!r}")
+    M, d = x.shape
+    dt = x.dtype if x.dtype in _CODES else torch.float16
+    ldx = _rows_of(x, "x", M, d, dt)
+    for t, name in ((gamma, "gamma"), (post_gamma, "post_gamma"), (gate, "gate")):
+        if t is not None and (t.shape != (d,) or t.dtype != dt or not t.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous [d] tensor of x's dtype")
+    if r is None and (h_out is not None or gate is not None or post_gamma is not None or alpha != 1.0):
+        raise ValueError("h_out, gate, post_gamma and alpha need r")
+    ldr = 0 if r is None else _rows_of(r, "r", M, d, dt)
+    ldh = d if h_out is None else _rows_of(h_out, "h_out", M, d, dt)
+    ldv = 0 if values is None else _rows_of(values, "values", M, d, dt)
+    _check(codes, "codes", (M, d // 2), torch.uint8)
+    if fmt == "mx4":
+        _check(scales, "scales", (M, mx4_scale_stride(d)), torch.uint8)
+    else:
+        _check(scales, "scales", (M,), torch.float32)
+    dev = x.device
+    if _elsewhere(x, gamma, r, post_gamma, gate, h_out, codes, scales, values):
+        with torch.cuda.device(dev):
+            return residual_rmsnorm_quant(x, gamma, r, eps, fmt, clip, post_gamma, gate, alpha, h_out, codes, scales,
+                                          values)
+    if r is not None and h_out is None:
+        h_out = torch.empty((M, d), dtype=dt, device=dev)
+    if fmt == "mx4":
+        codes, scales = _mx4_out(codes, scales, M, d, dev)
+    else:
+        if codes is None:
+            codes = torch.empty((M, d // 2), dtype=torch.uint8, device=dev)
+        if scales is None:
+            scales = torch.empty((M,), dtype=torch.float32, device=dev)
+    check(lib().p4q_residual_rmsnorm_quant(
+        _CODES[dt], P4Q_NORM_MX4 if fmt == "mx4" else P4Q_NORM_INT4, M, d, x.data_ptr(), ldx, _ptr(r), ldr,
+        _ptr(post_gamma), _ptr(gate), alpha, gamma.data_ptr(), eps, clip, _ptr(h_out), ldh, codes.data_ptr(),
+        scales.data_ptr(), _ptr(values), ldv, _stream(dev)))
+    return codes, scales, x if r is None else h_out
+
+
+def _mx4_product(fn: str, pair: int, a_codes, a_scales, w_codes, w_scales, out_dtype, y):
+    M, K = _mx4_rows(a_codes, a_scales, "a")
+    rows, K2 = _mx4_rows(w_codes, w_scales, "w")
+    if K != K2:
+        raise ValueError("a_codes and w_codes disagree on K")
+    if rows % pair:
+        raise ValueError(f"w_codes must hold gate rows and as many up rows, got {rows}")
+    N = rows // pair
+    if y is None:
+        if out_dtype not in _CODES:
+            raise ValueError(f"out_dtype must be fp16 or bf16, got {out_dtype}")
+    else:
+        _check_rows(y, "y", M, N, _F16)
+    dev = a_codes.device
+    if _elsewhere(a_codes, a_scales, w_codes, w_scales, y):
+        with torch.cuda.device(dev):
+            return _mx4_product(fn, pair, a_codes, a_scales, w_codes, w_scales, out_dtype, y)
+    if y is None:
+        y = torch.empty((M, N), dtype=out_dtype, device=dev)
+    check(getattr(lib(), fn)(M, N, K, a_codes.data_ptr(), a_scales.data_ptr(), w_codes.data_ptr(), w_scales.data_ptr(),
+                             _CODES[y.dtype], y.data_ptr(), y.stride(0) if M > 1 else max(N, y.stride(0)), _stream(dev)))
+    return y
+
+
+def mx4_linear(a_codes: torch.Tensor, a_scales: torch.Tensor, w_codes: torch.Tensor, w_scales: torch.Tensor,
+               out_dtype: torch.dtype = torch.bfloat16, y: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """MXFP4 linear (p4q_mx4_linear): a (codes [M, K/2], scales) and w (codes
+    [N, K/2], scales) as quant_mx4() gives them -> y [M, N] of out_dtype (of y's, if
+    given; its rows may be columns of a wider buffer)."""
+    return _mx4_product("p4q_mx4_linear", 1, a_codes, a_scales, w_codes, w_scales, out_dtype, y)
+
+
+def mx4_gated_linear(a_codes: torch.Tensor, a_scales: torch.Tensor, w_codes: torch.Tensor, w_scales: torch.Tensor,
+                     out_dtype: torch.dtype = torch.bfloat16, y: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Gate and up projection of a feed-forward block in one product
+    (p4q_mx4_gated_linear): w holds the gate's N rows, then the up projection's N;
+    y [M, N] = SiLU(a w_gate^T) * (a w_up^T)."""
+    return _mx4_product("p4q_mx4_gated_linear", 2, a_codes, a_scales, w_codes, w_scales, out_dtype, y)
+
+
+def mx4_gated_linear_quant(a_codes: torch.Tensor, a_scales: torch.Tensor, w_codes: torch.Tensor,
+                           w_scales: torch.Tensor, codes: Optional[torch.Tensor] = None,
+                           scales: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """mx4_gated_linear() whose result leaves as MXFP4 (p4q_mx4_gated_linear_quant),
+    ready for mx4_linear(): (codes uint8 [M, N/2], scales uint8
+    [M, mx4_scale_stride(N)]), N a multiple of 32."""
+    M, K = _mx4_rows(a_codes, a_scales, "a")
+    rows, K2 = _mx4_rows(w_codes, w_scales, "w")
+    if K != K2:
+        raise ValueError("a_codes and w_codes disagree on K")
+    if rows % 2:
+        raise ValueError(f"w_codes must hold gate rows and as many up rows, got {rows}")
+    N = rows // 2
+    _check(codes, "codes", (M, N // 2), torch.uint8)
+    _check(scales, "scales", (M, mx4_scale_stride(N)), torch.uint8)
+    dev = a_codes.device
+    if _elsewhere(a_codes, a_scales, w_codes, w_scales, codes, scales):
+        with torch.cuda.device(dev):
+            return mx4_gated_linear_quant(a_codes, a_scales, w_codes, w_scales, codes, scales)
+    codes, scales = _mx4_out(codes, scales, M, N, dev)
+    check(lib().p4q_mx4_gated_linear_quant(M, N, K, a_codes.data_ptr(), a_scales.data_ptr(), w_codes.data_ptr(),
+                                           w_scales.data_ptr(), codes.data_ptr(), scales.data_ptr(), _stream(dev)))
+    return codes, scales
 
 
 # --------------------------------------------------------------------------- diagnostics

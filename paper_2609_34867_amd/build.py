@@ -21,7 +21,8 @@ LIB_PATH = os.path.join(PKG_DIR, "libp4q.so")
 
 SOURCES = ["p4q_api.hip", "quant_act.hip", "prologue.hip", "select.hip", "diversity.hip", "calib.hip",
            "w4a4_gemm.hip", "w4a4_f6.hip", "attention.hip", "rope_append.hip",
-           "prompt_attention.hip", "decode_attention.hip", "diag.hip"]
+           "prompt_attention.hip", "decode_attention.hip", "quant_mx4.hip", "residual_norm.hip", "mx4_gemm.hip",
+           "diag.hip"]
 
 ARCH = "gfx950"
 HIPCC_FLAGS = [

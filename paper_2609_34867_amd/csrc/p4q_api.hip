@@ -526,6 +526,134 @@ int p4q_w4a4_linear(int M, int N_out, int K_in, const uint8_t *a_codes, const fl
                       "p4q_w4a4_linear");
 }
 
+// ---- MXFP4 -------------------------------------------------------------------
+size_t p4q_mx4_scale_stride(int K) {
+    if (K < 32 || K > 131072 || K % 32 != 0) return 0;
+    return (size_t)p4q::mx4_scale_stride(K);
+}
+
+// A 16-bit operand's rows: 16-byte aligned and at least `width` apart.
+static bool rows_ok(const void *p, int64_t ld, int width) { return aligned(p, 16) && ld >= width && ld % 8 == 0; }
+
+int p4q_quant_mx4(p4q_dtype dt, int M, int K, const void *x, int64_t ldx, uint8_t *codes,
+                  uint8_t *scales, void *values, int64_t ldv, hipStream_t stream) {
+    if (!valid_dtype(dt)) return fail(P4Q_ERR_UNSUPPORTED, "p4q_quant_mx4: dtype %d", (int)dt);
+    if (M <= 0 || K <= 0 || K % 32 != 0)
+        return fail(P4Q_ERR_INVALID_ARG, "p4q_quant_mx4: M=%d K=%d (K a multiple of 32)", M, K);
+    if (K > 131072 || M * ((K + 511LL) / 512) >= (1LL << 26))
+        return fail(P4Q_ERR_UNSUPPORTED, "p4q_quant_mx4: M=%d K=%d too large", M, K);
+    if (!x || !codes || !scales) return fail(P4Q_ERR_INVALID_ARG, "p4q_quant_mx4: null pointer");
+    if (!rows_ok(x, ldx, K) || (values && !rows_ok(values, ldv, K)))
+        return fail(P4Q_ERR_INVALID_ARG, "p4q_quant_mx4: ldx=%lld ldv=%lld (need >= K, multiples of 8; 16-byte aligned rows)",
+                    (long long)ldx, (long long)ldv);
+    if (!aligned(codes, 16) || !aligned(scales, 16)) return fail(P4Q_ERR_INVALID_ARG, "p4q_quant_mx4: misaligned pointer");
+    return hip_status(p4q::launch_quant_mx4(dt, M, K, x, ldx, codes, scales, values, ldv, stream), "p4q_quant_mx4");
+}
+
+static int check_mx4_product(const char *who, int M, int N_out, int K, const uint8_t *a_codes,
+                             const uint8_t *a_scales, const uint8_t *w_codes, const uint8_t *w_scales) {
+    if (M <= 0 || N_out <= 0 || K <= 0 || K % 32 != 0)
+        return fail(P4Q_ERR_INVALID_ARG, "%s: M=%d N_out=%d K=%d (K a multiple of 32)", who, M, N_out, K);
+    if (M > (1 << 20) || N_out > (1 << 22) || K > 131072)
+        return fail(P4Q_ERR_UNSUPPORTED, "%s: M=%d N_out=%d K=%d too large", who, M, N_out, K);
+    if (!a_codes || !a_scales || !w_codes || !w_scales) return fail(P4Q_ERR_INVALID_ARG, "%s: null pointer", who);
+    if (!aligned(a_codes, 16) || !aligned(a_scales, 16) || !aligned(w_codes, 16) || !aligned(w_scales, 16))
+        return fail(P4Q_ERR_INVALID_ARG, "%s: misaligned pointer", who);
+    return P4Q_OK;
+}
+
+static int check_mx4_output(const char *who, p4q_dtype out_dt, const void *y, int64_t ldy, int N_out) {
+    if (!valid_dtype(out_dt)) return fail(P4Q_ERR_UNSUPPORTED, "%s: dtype %d", who, (int)out_dt);
+    if (!y || !aligned(y, 4)) return fail(P4Q_ERR_INVALID_ARG, "%s: y null or misaligned", who);
+    if (ldy < N_out) return fail(P4Q_ERR_INVALID_ARG, "%s: ldy=%lld < N_out", who, (long long)ldy);
+    return P4Q_OK;
+}
+
+static p4q::Mx4Product mx4_product(int M, int N_out, int K, const uint8_t *a_codes, const uint8_t *a_scales,
+                                   const uint8_t *w_codes, const uint8_t *w_scales) {
+    p4q::Mx4Product p = {};
+    p.M = M, p.N = N_out, p.K = K;
+    p.a = a_codes, p.as = a_scales, p.w = w_codes, p.ws = w_scales;
+    return p;
+}
+
+int p4q_mx4_linear(int M, int N_out, int K, const uint8_t *a_codes, const uint8_t *a_scales,
+                   const uint8_t *w_codes, const uint8_t *w_scales, p4q_dtype out_dt, void *y,
+                   int64_t ldy, hipStream_t stream) {
+    const char *who = "p4q_mx4_linear";
+    if (const int st = check_mx4_product(who, M, N_out, K, a_codes, a_scales, w_codes, w_scales)) return st;
+    if (const int st = check_mx4_output(who, out_dt, y, ldy, N_out)) return st;
+    p4q::Mx4Product p = mx4_product(M, N_out, K, a_codes, a_scales, w_codes, w_scales);
+    p.y = y, p.ldy = ldy;
+    return hip_status(p4q::launch_mx4_linear(out_dt, p, stream), who);
+}
+
+int p4q_mx4_gated_linear(int M, int N_out, int K, const uint8_t *a_codes, const uint8_t *a_scales,
+                         const uint8_t *w_codes, const uint8_t *w_scales, p4q_dtype out_dt, void *y,
+                         int64_t ldy, hipStream_t stream) {
+    const char *who = "p4q_mx4_gated_linear";
+    if (const int st = check_mx4_product(who, M, N_out, K, a_codes, a_scales, w_codes, w_scales)) return st;
+    if (const int st = check_mx4_output(who, out_dt, y, ldy, N_out)) return st;
+    p4q::Mx4Product p = mx4_product(M, N_out, K, a_codes, a_scales, w_codes, w_scales);
+    p.y = y, p.ldy = ldy;
+    return hip_status(p4q::launch_mx4_gated(out_dt, p, stream), who);
+}
+
+int p4q_mx4_gated_linear_quant(int M, int N_out, int K, const uint8_t *a_codes,
+                               const uint8_t *a_scales, const uint8_t *w_codes,
+                               const uint8_t *w_scales, uint8_t *codes, uint8_t *scales,
+                               hipStream_t stream) {
+    const char *who = "p4q_mx4_gated_linear_quant";
+    if (const int st = check_mx4_product(who, M, N_out, K, a_codes, a_scales, w_codes, w_scales)) return st;
+    if (N_out % 32 != 0) return fail(P4Q_ERR_INVALID_ARG, "%s: N_out=%d not a multiple of 32", who, N_out);
+    if (!codes || !scales || !aligned(codes, 16) || !aligned(scales, 16))
+        return fail(P4Q_ERR_INVALID_ARG, "%s: codes or scales null or misaligned", who);
+    p4q::Mx4Product p = mx4_product(M, N_out, K, a_codes, a_scales, w_codes, w_scales);
+    p.codes = codes, p.scales = scales;
+    return hip_status(p4q::launch_mx4_gated(P4Q_BF16, p, stream), who);
+}
+
+int p4q_residual_rmsnorm_quant(p4q_dtype dt, p4q_norm_format fmt, int M, int d, const void *x,
+                               int64_t ldx, const void *r, int64_t ldr, const void *post_gamma,
+                               const void *gate, float alpha, const void *gamma, float eps,
+                               float clip, void *h_out, int64_t ldh, uint8_t *codes, void *scales,
+                               void *values, int64_t ldv, hipStream_t stream) {
+    const char *who = "p4q_residual_rmsnorm_quant";
+    if (!valid_dtype(dt)) return fail(P4Q_ERR_UNSUPPORTED, "%s: dtype %d", who, (int)dt);
+    if (fmt != P4Q_NORM_INT4 && fmt != P4Q_NORM_MX4) return fail(P4Q_ERR_UNSUPPORTED, "%s: format %d", who, (int)fmt);
+    if (M <= 0 || d <= 0 || d % 32 != 0) return fail(P4Q_ERR_INVALID_ARG, "%s: M=%d d=%d (d a multiple of 32)", who, M, d);
+    if (d > 16384 || M >= (1 << 23)) return fail(P4Q_ERR_UNSUPPORTED, "%s: M=%d d=%d too large", who, M, d);
+    if (!x || !gamma || !codes || !scales) return fail(P4Q_ERR_INVALID_ARG, "%s: null pointer", who);
+    if (!r && (h_out || gate || post_gamma || alpha != 1.0f))
+        return fail(P4Q_ERR_INVALID_ARG, "%s: h_out, gate, post_gamma and alpha need r", who);
+    if (r && !h_out) return fail(P4Q_ERR_INVALID_ARG, "%s: r needs h_out", who);
+    if (!rows_ok(x, ldx, d) || (r && (!rows_ok(r, ldr, d) || !rows_ok(h_out, ldh, d))) ||
+        (values && !rows_ok(values, ldv, d)))
+        return fail(P4Q_ERR_INVALID_ARG, "%s: row strides %lld %lld %lld %lld (need >= d, multiples of 8; 16-byte aligned rows)",
+                    who, (long long)ldx, (long long)ldr, (long long)ldh, (long long)ldv);
+    if (r && ((h_out == x && ldh != ldx) || (h_out == r && ldh != ldr)))
+        return fail(P4Q_ERR_INVALID_ARG, "%s: h_out in place needs the same row stride", who);
+    if (!aligned(gamma, 16) || !aligned(codes, 16) || (post_gamma && !aligned(post_gamma, 16)) ||
+        (gate && !aligned(gate, 16)) || !aligned(scales, fmt == P4Q_NORM_MX4 ? 16 : 4))
+        return fail(P4Q_ERR_INVALID_ARG, "%s: misaligned pointer", who);
+    if (!(eps >= 0.0f && eps <= 1.0f)) return fail(P4Q_ERR_INVALID_ARG, "%s: eps %g outside [0, 1]", who, eps);
+    if (!(alpha - alpha == 0.0f)) return fail(P4Q_ERR_INVALID_ARG, "%s: alpha %g", who, alpha);
+    if (!valid_clip(clip) || (fmt == P4Q_NORM_MX4 && clip != 1.0f))
+        return fail(P4Q_ERR_INVALID_ARG, "%s: clip %g (int4: in [2^-16, 1]; MXFP4: 1)", who, clip);
+    p4q::ResidualNorm a = {};
+    a.M = M, a.d = d;
+    a.x = static_cast<const uint16_t *>(x), a.ldx = ldx;
+    a.r = static_cast<const uint16_t *>(r), a.ldr = ldr;
+    a.post = static_cast<const uint16_t *>(post_gamma);
+    a.gate = static_cast<const uint16_t *>(gate);
+    a.gamma = static_cast<const uint16_t *>(gamma);
+    a.alpha = alpha, a.eps = eps, a.clip = clip;
+    a.h_out = static_cast<uint16_t *>(h_out), a.ldh = ldh;
+    a.codes = codes, a.scales = scales;
+    a.values = static_cast<uint16_t *>(values), a.ldv = ldv;
+    return hip_status(p4q::launch_residual_rmsnorm_quant(dt, fmt, a, stream), who);
+}
+
 int p4q_quant_scaled(p4q_dtype dt, int R, int K, const void *z, int64_t ldz, const float *sigma,
                      int divide, float clip, const float *clip_rows, uint8_t *codes,
                      float *scales, float *absmax, int32_t *kstar, hipStream_t stream) {

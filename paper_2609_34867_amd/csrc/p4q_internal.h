@@ -61,6 +61,45 @@ hipError_t launch_rmsnorm_quant(p4q_dtype dt, int M, int d, const void *x, int64
                                 const void *gamma, float eps, float clip, uint8_t *codes,
                                 float *scales, hipStream_t stream);
 
+// ---- MXFP4: rows of 4-bit floats with one power of two per 32 ------------------
+// (mx4_device.h has the format.)  Fields behind `set by the launcher` are the
+// kernels' own.
+hipError_t launch_quant_mx4(p4q_dtype dt, int M, int K, const void *x, int64_t ldx, uint8_t *codes,
+                            uint8_t *scales, void *values, int64_t ldv, hipStream_t stream);
+
+// bytes of a row of scales: one byte per 32 values, padded to 16 bytes so that
+// rows start aligned and 512 values of a product find their 16 bytes
+__host__ __device__ inline int64_t mx4_scale_stride(int64_t K) { return (K + 511) / 512 * 16; }
+
+struct ResidualNorm {
+    int M, d;
+    const uint16_t *x, *r, *post, *gate, *gamma;     // r, post and gate may be null
+    int64_t ldx, ldr;
+    float alpha, eps, clip;
+    uint16_t *h_out;                                 // given iff r is
+    int64_t ldh;
+    uint8_t *codes;
+    void *scales;                                    // fp32 [M], or bytes [M, stride]
+    uint16_t *values;                                // may be null
+    int64_t ldv;
+    // set by the launcher
+    int64_t scale_stride;
+};
+hipError_t launch_residual_rmsnorm_quant(p4q_dtype dt, p4q_norm_format fmt, ResidualNorm a, hipStream_t stream);
+
+struct Mx4Product {
+    int M, N, K;                                     // N: outputs (gated: half the weight's rows)
+    const uint8_t *a, *as, *w, *ws;                  // codes and scale bytes
+    void *y;
+    int64_t ldy;
+    uint8_t *codes, *scales;                         // gated and quantized: instead of y
+    // set by the launcher
+    int64_t in_stride, out_stride;                   // bytes of a row of scales
+    bool wide;                                       // 16-byte stores to y
+};
+hipError_t launch_mx4_linear(p4q_dtype out_dt, Mx4Product p, hipStream_t stream);
+hipError_t launch_mx4_gated(p4q_dtype out_dt, Mx4Product p, hipStream_t stream);
+
 // ---- attention prefill (FP16 / BF16 Q, K, V; head dimension 128) -------------
 hipError_t launch_attention(p4q_dtype dt, int B, int L, int H, const void *q, const void *k,
                             const void *v, int64_t ld, void *o, int64_t ldo, int causal,

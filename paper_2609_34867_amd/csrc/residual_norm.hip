@@ -1,0 +1,227 @@
+// What lies between two blocks of a decoder layer, in one pass: the block's
+// output, normalized where the model does so and gated, is added to the
+// residual, and the next block's RMSNorm of the sum is quantized.
+//
+//   r' = post ? r / rms(r) * post : r
+//   h  = round16(fl32(x + alpha gate r'))            (no r: h = x)
+//   int4:  codes = Q4(u; clip), scale = fl32(s / rms(h)),  u = h gamma
+//   MXFP4: codes, scales of fl32(u / rms(h)), 32 values at a time
+//   rms(z) = sqrt(sum z^2 / d + eps)
+//
+// The sums of squares, their roots and what is multiplied by them are held in
+// 64 bits: an MXFP4 code is decided by a value that 1 / rms scales, and the one
+// rounding to fp32 is then that of the definition whatever the order of the
+// sum.  (Its arithmetic hides behind the memory.)  The int4 codes need no rms
+// at all: they are those of u, exact in fp32, as in the prologue without a
+// residual.
+//
+// One work-group per row, which stays in registers from the load to the
+// codes: x and r are read once, h, the codes and the scales written once.
+#include "mx4_device.h"
+#include "p4q_internal.h"
+#include "q4_device.h"
+
+namespace p4q {
+namespace {
+
+constexpr int kThreads = 256;
+
+__device__ __forceinline__ double block_sum(double s, double *buf) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
+    if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = s;
+    __syncthreads();
+    double t = 0.0;
+#pragma unroll
+    for (int i = 0; i < kThreads / 64; ++i) t += buf[i];
+    return t;
+}
+
+// 1 / rms of a row; a row of zeros at eps = 0 stays one of zeros
+__device__ __forceinline__ double inverse_rms(double ss, int d, float eps) {
+    const double ms = ss / (double)d + (double)eps;
+    return ms == 0.0 ? 0.0 : 1.0 / __builtin_sqrt(ms);
+}
+
+template <bool BF16>
+__device__ __forceinline__ void unpack8(uint4 w, float (&v)[8]) {
+    const uint32_t xw[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = lo_f32<BF16>(xw[i]);
+        v[2 * i + 1] = hi_f32<BF16>(xw[i]);
+    }
+}
+
+template <int CH, bool BF16, bool INT4, bool CLIP1>
+__global__ __launch_bounds__(kThreads) void k_residual_rmsnorm_quant(const ResidualNorm a) {
+    __shared__ double s_r[kThreads / 64], s_h[kThreads / 64];
+    __shared__ uint32_t s_max[kThreads / 64];
+    const int64_t row = blockIdx.x;
+    const int t = threadIdx.x;
+    const int chunks = a.d / 8;
+    const uint4 zero = make_uint4(0, 0, 0, 0);
+    auto row_of = [&](const uint16_t *p, int64_t ld) { return reinterpret_cast<const uint4 *>(p + row * ld); };
+
+    uint4 h[CH], r[CH], g[CH];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int q = t + kThreads * c;
+        const bool in = q < chunks;
+        h[c] = in ? load_nt(row_of(a.x, a.ldx) + q) : zero;
+        r[c] = in && a.r ? load_nt(row_of(a.r, a.ldr) + q) : zero;
+        g[c] = in ? reinterpret_cast<const uint4 *>(a.gamma)[q] : zero;
+    }
+    if (a.r) {
+        double inv = 0.0;
+        if (a.post) {
+            double ss = 0.0;
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                float v[8];
+                unpack8<BF16>(r[c], v);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) ss = __builtin_fma((double)v[i], (double)v[i], ss);
+            }
+            ss = block_sum(ss, s_r);
+            inv = inverse_rms(ss, a.d, a.eps);
+        }
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int q = t + kThreads * c;
+            if (q >= chunks) continue;
+            float x[8], v[8], p[8], e[8], o[8];
+            unpack8<BF16>(h[c], x);
+            unpack8<BF16>(r[c], v);
+            if (a.post) unpack8<BF16>(reinterpret_cast<const uint4 *>(a.post)[q], p);
+            if (a.gate) unpack8<BF16>(reinterpret_cast<const uint4 *>(a.gate)[q], e);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                double z = (double)v[i];
+                if (a.post) z = z * inv * (double)p[i];
+                if (a.gate) z *= (double)e[i];
+                o[i] = (float)((double)x[i] + (double)a.alpha * z);
+            }
+            h[c] = round16x8<BF16>(o);
+            reinterpret_cast<uint4 *>(a.h_out + row * a.ldh)[q] = h[c];
+        }
+    }
+
+    double ss = 0.0;
+    float am = 0.0f;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        float v[8], w[8];
+        unpack8<BF16>(h[c], v);
+        if constexpr (INT4) unpack8<BF16>(g[c], w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            ss = __builtin_fma((double)v[i], (double)v[i], ss);
+            if constexpr (INT4) am = __builtin_fmaxf(am, __builtin_fabsf(v[i] * w[i]));
+        }
+    }
+    if constexpr (INT4) {
+        const uint32_t mw = wave_max_u32(__float_as_uint(am));
+        if ((t & 63) == 0) s_max[t >> 6] = mw;
+    }
+    ss = block_sum(ss, s_h);
+    const double inv = inverse_rms(ss, a.d, a.eps);
+
+    if constexpr (INT4) {
+        const float top = __uint_as_float(max(max(s_max[0], s_max[1]), max(s_max[2], s_max[3])));
+        const float s = row_scale<CLIP1>(top, a.clip);
+        const float scale = s == 0.0f ? 0.0f : (float)((double)s * inv);
+        if (t == 0) static_cast<float *>(a.scales)[row] = scale;
+        const bool tiny = !(s >= kTinyScale);
+        const float rs = tiny ? 0.0f : 1.0f / s;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int q = t + kThreads * c;
+            float u[8], w8[8];
+            unpack8<BF16>(h[c], u);
+            unpack8<BF16>(g[c], w8);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) u[i] = u[i] * w8[i];
+            uint32_t w[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+            uint32_t near = 0;
+            if (s != 0.0f) {
+                if (!tiny) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) w[k] = q4_fast<CLIP1>(u[k], rs, near);
+                }
+                if (tiny || __any((int)near)) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        float uk = u[k];
+                        asm volatile("" : "+v"(uk));
+                        w[k] = q4_exact(uk, s);
+                    }
+                }
+            }
+            const uint32_t packed = pack_nibbles(w);
+            if (q < chunks) {
+                reinterpret_cast<uint32_t *>(a.codes)[row * chunks + q] = packed;
+                if (a.values) {
+                    float v[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) v[k] = (float)((int)(packed << (28 - 4 * k)) >> 28) * scale;
+                    reinterpret_cast<uint4 *>(a.values + row * a.ldv)[q] = round16x8<BF16>(v);
+                }
+            }
+        }
+    } else {
+        uint8_t *scales = static_cast<uint8_t *>(a.scales) + row * a.scale_stride;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int q = t + kThreads * c;
+            float u[8], w8[8];
+            unpack8<BF16>(h[c], u);
+            unpack8<BF16>(g[c], w8);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) u[i] = (float)((double)u[i] * (double)w8[i] * inv);
+            uint32_t byte;
+            const uint32_t packed = mx4_quantize(u, byte);
+            if (q < chunks) {
+                if ((t & 3) == 0) scales[q >> 2] = (uint8_t)byte;
+                reinterpret_cast<uint32_t *>(a.codes)[row * chunks + q] = packed;
+                if (a.values) {
+                    mx4_values(packed, byte, u);
+                    reinterpret_cast<uint4 *>(a.values + row * a.ldv)[q] = round16x8<BF16>(u);
+                }
+            }
+        }
+        const int pad = a.d / 32 + t;                    // the row's padding
+        if (pad < (int)a.scale_stride) scales[pad] = 0;
+    }
+}
+
+template <int CH, bool BF16>
+hipError_t launch_ch(p4q_norm_format fmt, const ResidualNorm &a, hipStream_t stream) {
+    auto go = [&](auto kern) {
+        hipLaunchKernelGGL(kern, dim3(a.M), dim3(kThreads), 0, stream, a);
+        return hipGetLastError();
+    };
+    if (fmt == P4Q_NORM_MX4) return go(k_residual_rmsnorm_quant<CH, BF16, false, true>);
+    return a.clip == 1.0f ? go(k_residual_rmsnorm_quant<CH, BF16, true, true>)
+                          : go(k_residual_rmsnorm_quant<CH, BF16, true, false>);
+}
+
+template <bool BF16>
+hipError_t launch_typed(p4q_norm_format fmt, const ResidualNorm &a, hipStream_t stream) {
+    const int per = (a.d / 8 + kThreads - 1) / kThreads;  // d <= 16384: at most 8
+    if (per <= 1) return launch_ch<1, BF16>(fmt, a, stream);
+    if (per <= 2) return launch_ch<2, BF16>(fmt, a, stream);
+    if (per <= 3) return launch_ch<3, BF16>(fmt, a, stream);
+    if (per <= 4) return launch_ch<4, BF16>(fmt, a, stream);
+    if (per <= 6) return launch_ch<6, BF16>(fmt, a, stream);
+    return launch_ch<8, BF16>(fmt, a, stream);
+}
+
+}  // namespace
+
+hipError_t launch_residual_rmsnorm_quant(p4q_dtype dt, p4q_norm_format fmt, ResidualNorm a, hipStream_t stream) {
+    a.scale_stride = mx4_scale_stride(a.d);
+    return dt == P4Q_BF16 ? launch_typed<true>(fmt, a, stream) : launch_typed<false>(fmt, a, stream);
+}
+
+}  // namespace p4q
