@@ -27,6 +27,41 @@ __device__ __forceinline__ float mx4_scale(uint32_t byte) {
     return __uint_as_float(byte == 0 ? 0x00400000u : byte << 23);
 }
 
+// the scale byte of a block whose largest magnitude has these bits (255: not finite)
+__device__ __forceinline__ uint32_t mx4_byte(uint32_t top) {
+    const uint32_t e = top >> 23;
+    return e == 255u ? 255u : max(e, 2u) - 2u;
+}
+
+// 1 / X of a scale byte below 255
+__device__ __forceinline__ float mx4_inverse(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
+
+// four codes (value i in nibble i) of values already divided by X
+__device__ __forceinline__ uint32_t mx4_codes4(float a, float b, float c, float d) {
+    uint32_t w = 0;
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, a, b, 1.0f, 0);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, c, d, 1.0f, 1);
+}
+
+// Quantizes a block that lanes l and l + 32 hold, 16 values each: lane l the
+// values 8 g + 0..3, lane l + 32 the values 8 g + 4..7, in v[4 g ..].  Returns 8
+// bytes of codes, lane l the block's first half, lane l + 32 its second.
+__device__ __forceinline__ uint2 mx4_quantize_halves(const float (&v)[16], uint32_t &byte) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+    top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+    byte = mx4_byte(top);
+    const float inv = byte == 255u ? 0.0f : mx4_inverse(byte);
+    uint32_t c[4];
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+        c[g] = byte == 255u ? 0u : mx4_codes4(v[4 * g] * inv, v[4 * g + 1] * inv, v[4 * g + 2] * inv, v[4 * g + 3] * inv);
+    // the upper lanes' groups 0 and 1 against the lower lanes' 2 and 3
+    const auto s = __builtin_amdgcn_permlane32_swap(c[0] | (c[1] << 16), c[2] | (c[3] << 16), false, false);
+    return make_uint2((s[0] & 0xFFFFu) | (s[1] << 16), (s[0] >> 16) | (s[1] & 0xFFFF0000u));
+}
+
 // Quantizes a block that the four lanes of a quad hold, 8 consecutive values
 // each.  Returns this lane's 8 codes (value i in nibble i) and, in every lane,
 // the block's scale byte.
@@ -36,19 +71,11 @@ __device__ __forceinline__ uint32_t mx4_quantize(const float (&v)[8], uint32_t &
     for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
     top = max(top, lane_xor<1>(top));
     top = max(top, lane_xor<2>(top));
-    const uint32_t e = top >> 23;
-    byte = max(e, 2u) - 2u;
-    const float inv = __uint_as_float((254u - byte) << 23);
-    uint32_t c = 0;
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[0] * inv, v[1] * inv, 1.0f, 0);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[2] * inv, v[3] * inv, 1.0f, 1);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[4] * inv, v[5] * inv, 1.0f, 2);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[6] * inv, v[7] * inv, 1.0f, 3);
-    if (e == 255u) {
-        byte = 255u;
-        c = 0;
-    }
-    return c;
+    byte = mx4_byte(top);
+    if (byte == 255u) return 0;
+    const float inv = mx4_inverse(byte);
+    return mx4_codes4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv) |
+           (mx4_codes4(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv) << 16);
 }
 
 // The 8 values that codes and a scale byte stand for.

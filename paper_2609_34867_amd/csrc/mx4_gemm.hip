@@ -14,6 +14,7 @@
 
 #include <algorithm>
 #include <type_traits>
+#include <utility>
 
 namespace p4q {
 namespace {
@@ -34,6 +35,20 @@ __device__ __forceinline__ void mfma_mx4(v4i w, uint32_t sw, v4i a, uint32_t sa,
 
 __device__ __forceinline__ float silu(float g) { return g / (1.0f + __expf(-g)); }
 
+// 8 consecutive 16-bit outputs n0 .. n0 + 7 of row m, as far as they exist
+__device__ __forceinline__ void store8(const Mx4Product &p, int64_t m, int n0, uint4 w) {
+    if (m >= p.M || n0 >= p.N) return;
+    uint16_t *dst = static_cast<uint16_t *>(p.y) + m * p.ldy + n0;
+    if (p.wide && n0 + 8 <= p.N) {
+        *reinterpret_cast<uint4 *>(dst) = w;
+    } else {
+        const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (n0 + i < p.N) dst[i] = (uint16_t)(x[i >> 1] >> (16 * (i & 1)));
+    }
+}
+
 // 8 consecutive outputs n0 .. n0 + 7 of row m (u: the up sums, gated only).
 // Four lanes of a quad hold 32 outputs of one row in order.
 template <int EPI, bool BF16>
@@ -50,17 +65,7 @@ __device__ __forceinline__ void emit8(const Mx4Product &p, int64_t m, int n0, fl
             if ((n0 & 31) == 0) p.scales[m * p.out_stride + (n0 >> 5)] = (uint8_t)byte;
         }
     } else {
-        if (m >= p.M || n0 >= p.N) return;
-        uint16_t *dst = static_cast<uint16_t *>(p.y) + m * p.ldy + n0;
-        const uint4 w = round16x8<BF16>(v);
-        if (p.wide && n0 + 8 <= p.N) {
-            *reinterpret_cast<uint4 *>(dst) = w;
-        } else {
-            const uint32_t x[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (n0 + i < p.N) dst[i] = (uint16_t)(x[i >> 1] >> (16 * (i & 1)));
-        }
+        store8(p, m, n0, round16x8<BF16>(v));
     }
 }
 
@@ -176,8 +181,282 @@ __global__ __launch_bounds__(64 * kSkinnyWaves) void k_mx4_skinny(const Mx4Produ
     }
 }
 
+// ---- tiles through LDS -----------------------------------------------------------
+// A work-group of four wavefronts, 2 x 2, computes 64 FM rows by 64 FN weight
+// rows, each wavefront FM x FN fragments of 32 x 32.  k runs in stages of 256
+// values; a ring of two stages in LDS is filled by DMA and runs on across the
+// tiles of a persistent work-group.
+//  * A stage's row is 128 bytes, one cache line, loaded by 8 lanes.  Chunk c of
+//    16 bytes (32 codes) of row r lies at c ^ (r % 8), so that the 32 rows of a
+//    fragment read fall into distinct banks.
+//  * The operands of a 64-value step are read while the step before it is
+//    multiplied.  The last step of a stage waits for the next stage's DMA and for
+//    every wavefront to hold this one's last operands; from there the slot takes
+//    the stage after the next.
+//  * Past the row's end the DMA's offsets lie outside the buffer and give codes
+//    of zero, and the scale bytes there are masked; rows past the last are outside
+//    it too.
+template <class F, int... I>
+__device__ __forceinline__ void unrolled_seq(F &&f, std::integer_sequence<int, I...>) {
+    (f(std::integral_constant<int, I>{}), ...);
+}
+// f(0) .. f(N - 1), the arguments compile-time constants
+template <int N, class F>
+__device__ __forceinline__ void unrolled(F &&f) {
+    unrolled_seq(f, std::make_integer_sequence<int, N>{});
+}
+
+constexpr int kRowBytes = 128;                   // codes of a row in a stage
+constexpr int kRowScales = 8;
+
+template <int EPI, bool BF16, int FM, int FN>
+__global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void k_mx4_tile(const Mx4Product p, int tiles_m, int tiles_n) {
+    constexpr int BM = 64 * FM, BW = 64 * FN;              // rows of a, of w
+    constexpr int BN = EPI == kLinear ? BW : BW / 2;       // outputs: half of w's rows are the gate's
+    constexpr int FO = EPI == kLinear ? FN : FN / 2;       // fragments of outputs per wavefront
+    constexpr int OFF_W = BM * kRowBytes, OFF_SA = OFF_W + BW * kRowBytes, OFF_SW = OFF_SA + BM * kRowScales;
+    constexpr int STAGE = OFF_SW + BW * kRowScales;
+    constexpr int EW = FO >= 2 && FM * FN >= 16 ? 2 : 1;                    // fragments stored together
+    constexpr int OUT_ROW = 64 * EW, OUT_WAVE = EPI == kGatedQuant ? 0 : 32 * OUT_ROW;
+    constexpr int CODE_DMAS = 2 * (FM + FN), SCALE_DMAS = (FM + FN) / 2, DMAS = CODE_DMAS + SCALE_DMAS;
+    static_assert(EPI == kLinear || FN % 2 == 0, "gate and up fragments");
+    static_assert((FM + FN) % 2 == 0, "scale loads");
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * STAGE + 4 * OUT_WAVE];
+
+    const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int wm = wave & 1, wn = wave >> 1;
+    const int blocks = p.K / 32, KT = (blocks + 7) / 8;
+    const uint32_t kb = (uint32_t)p.K / 2, sb = (uint32_t)p.in_stride;
+
+    // this work-group's tiles: a contiguous share of its XCD's range
+    const int T = tiles_m * tiles_n;
+    const int xcd = blockIdx.x % kXcds, i0 = blockIdx.x / kXcds;
+    const int nb = ((int)gridDim.x - xcd + kXcds - 1) / kXcds;
+    const int q = T / kXcds, rr = T % kXcds;
+    const int start = (xcd < rr) ? xcd * (q + 1) : rr * (q + 1) + (xcd - rr) * q;
+    const int len = q + (xcd < rr ? 1 : 0);
+    const int nt = (i0 < len) ? (len - i0 + nb - 1) / nb : 0;
+    if (nt == 0) return;                                   // block-uniform
+    auto tile_at = [&](int k, int &tm, int &tn) __attribute__((always_inline)) {
+        grouped_tile(start + i0 + k * nb, tiles_m, tiles_n, tm, tn);
+    };
+
+    // ---- DMA: one stage is issue_begin(), then issue(i) for i < DMAS
+    const uint32_t lds = lds_addr(smem);
+    const uint32_t c_row = (uint32_t)lane >> 3, c_chunk = ((uint32_t)lane & 7u) ^ c_row;
+    const uint32_t v_codes = c_row * kb + c_chunk * 16u;
+    const uint32_t v_scales = ((uint32_t)lane >> 1) * sb + ((uint32_t)lane & 1u) * 4u;
+    constexpr uint32_t kOutside = 0x80000000u;
+    int iss_tile = -1, iss_kt = KT - 1, iss_slot = 1;
+    v4i dA = {}, dW = {}, dSA = {}, dSG = {}, dSU = {};
+    uint32_t iss_v = 0, iss_s = 0, iss_lds = 0;
+    auto issue_begin = [&]() __attribute__((always_inline)) {
+        if (++iss_kt == KT) {
+            iss_kt = 0;
+            ++iss_tile;
+            const bool live = iss_tile < nt;               // past the last tile: empty buffers
+            int tm = 0, tn = 0;
+            if (live) tile_at(iss_tile, tm, tn);
+            const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
+            const uint32_t ra = live ? (uint32_t)min((int64_t)p.M - m0, (int64_t)BM) : 0u;
+            const uint32_t rw = live ? (uint32_t)min((int64_t)p.N - n0, (int64_t)BN) : 0u;
+            const int64_t up = EPI == kLinear ? 0 : p.N;   // the up rows' distance
+            dA = buffer_desc(p.a + m0 * kb, ra * kb);
+            dSA = buffer_desc(p.as + m0 * sb, ra * sb);
+            dW = buffer_desc(p.w + (n0 + (wave >= 2 ? up : 0)) * kb, rw * kb);
+            dSG = buffer_desc(p.ws + n0 * sb, rw * sb);
+            dSU = buffer_desc(p.ws + (n0 + up) * sb, rw * sb);
+        }
+        iss_slot ^= 1;
+        iss_lds = lds + (uint32_t)iss_slot * STAGE;
+        iss_v = (uint32_t)iss_kt * 8u + c_chunk < (uint32_t)blocks ? v_codes + (uint32_t)iss_kt * kRowBytes : kOutside;
+        iss_s = v_scales + (uint32_t)iss_kt * kRowScales;
+    };
+    auto issue = [&](auto i_c) __attribute__((always_inline)) {
+        constexpr int i = decltype(i_c)::value;
+        if constexpr (i < 2 * FM) {                        // 8 rows of a
+            const uint32_t g = (uint32_t)(wave * 2 * FM + i);
+            dma16(dA, iss_v + g * 8u * kb, iss_lds + g * 1024u);
+        } else if constexpr (i < CODE_DMAS) {              // 8 rows of w; wavefronts 2 and 3: the second half
+            const uint32_t g = (uint32_t)(wave * 2 * FN + i - 2 * FM);
+            const uint32_t row = EPI == kLinear ? g : (uint32_t)((wave & 1) * 2 * FN + i - 2 * FM);
+            dma16(dW, iss_v + row * 8u * kb, iss_lds + OFF_W + g * 1024u);
+        } else {                                           // the scales of 32 rows of a or w
+            const uint32_t g = (uint32_t)(wave * SCALE_DMAS + i - CODE_DMAS);
+            if (g < 2 * FM) {
+                dma4(dSA, iss_s + g * 32u * sb, iss_lds + OFF_SA + g * 256u);
+            } else {
+                const uint32_t w = g - 2 * FM;
+                const bool second = EPI != kLinear && w >= FN;
+                dma4(second ? dSU : dSG, iss_s + (second ? w - FN : w) * 32u * sb, iss_lds + OFF_SW + w * 256u);
+            }
+        }
+    };
+    auto issue_all = [&]() __attribute__((always_inline)) {
+        issue_begin();
+        unrolled<DMAS>(issue);
+    };
+
+    // ---- operands of a step
+    // (gated: a wavefront's first fragments are the gate's, the others the up rows' of the same outputs)
+    const int row_w = EPI == kLinear ? wn * 32 * FN : wn * 32 * FO;
+    auto w_row = [&](int f) { return EPI == kLinear || f < FO ? 32 * f : BN + 32 * (f - FO); };
+    uint32_t xo[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) xo[i] = (uint32_t)(r * kRowBytes + (((4 * h + i) ^ (r & 7)) << 4));
+    const uint32_t a_at = (uint32_t)(wm * 32 * FM * kRowBytes), w_at = (uint32_t)(OFF_W + row_w * kRowBytes);
+    const uint32_t sa_at = (uint32_t)(OFF_SA + (wm * 32 * FM + r) * kRowScales + 4 * h);
+    const uint32_t sw_at = (uint32_t)(OFF_SW + (row_w + r) * kRowScales + 4 * h);
+    v4i a[2][FM], w[2][FN];
+    uint32_t ra[FM], rw[FN], sa[FM], sw[FN];
+    auto read_step = [&](uint32_t slot, auto i_c, auto set_c) __attribute__((always_inline)) {
+        constexpr int i = decltype(i_c)::value, S = decltype(set_c)::value;
+        const uint8_t *b = smem + slot * STAGE + xo[i];
+#pragma unroll
+        for (int j = 0; j < FM; ++j) a[S][j] = *reinterpret_cast<const v4i *>(b + a_at + 32 * kRowBytes * j);
+#pragma unroll
+        for (int f = 0; f < FN; ++f) w[S][f] = *reinterpret_cast<const v4i *>(b + w_at + kRowBytes * w_row(f));
+    };
+    auto read_scales = [&](uint32_t slot) __attribute__((always_inline)) {
+        const uint8_t *b = smem + slot * STAGE;
+#pragma unroll
+        for (int j = 0; j < FM; ++j) ra[j] = *reinterpret_cast<const uint32_t *>(b + sa_at + 32 * kRowScales * j);
+#pragma unroll
+        for (int f = 0; f < FN; ++f) rw[f] = *reinterpret_cast<const uint32_t *>(b + sw_at + kRowScales * w_row(f));
+    };
+
+    issue_all();
+    issue_all();
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(DMAS) : "memory");
+    uint32_t slot = 0;
+    read_step(0, std::integral_constant<int, 0>{}, std::integral_constant<int, 0>{});
+    read_scales(0);
+
+    for (int ck = 0; ck < nt; ++ck) {
+        v16f acc[FN][FM];
+#pragma unroll
+        for (int f = 0; f < FN; ++f)
+#pragma unroll
+            for (int j = 0; j < FM; ++j) acc[f][j] = v16f{};
+        for (int kt = 0; kt < KT; ++kt) {
+            const int left = blocks - 8 * kt - 4 * h;
+            const uint32_t mask = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
+#pragma unroll
+            for (int j = 0; j < FM; ++j) sa[j] = ra[j] & mask;
+#pragma unroll
+            for (int f = 0; f < FN; ++f) sw[f] = rw[f] & mask;
+            auto step = [&](auto i_c) __attribute__((always_inline)) {
+                constexpr int i = decltype(i_c)::value, S = i & 1;
+                if constexpr (i < 3) {
+                    read_step(slot, std::integral_constant<int, i + 1>{}, std::integral_constant<int, 1 - S>{});
+                } else {
+                    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+                    slot ^= 1;
+                    issue_begin();
+                    read_step(slot, std::integral_constant<int, 0>{}, std::integral_constant<int, 0>{});
+                    read_scales(slot);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                unrolled<FM * FN>([&](auto x_c) __attribute__((always_inline)) {
+                    constexpr int x = decltype(x_c)::value, f = x / FM, j = x % FM;
+                    mfma_mx4<i>(w[S][f], sw[f], a[S][j], sa[j], acc[f][j]);
+                    if constexpr (i == 3) {                // the DMAs spread over the step's products
+                        constexpr int lo = x * DMAS / (FM * FN), hi = (x + 1) * DMAS / (FM * FN);
+                        unrolled<hi - lo>([&](auto d_c) __attribute__((always_inline)) {
+                            issue(std::integral_constant<int, lo + decltype(d_c)::value>{});
+                        });
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                });
+                __builtin_amdgcn_sched_barrier(0);
+            };
+            step(std::integral_constant<int, 0>{});
+            step(std::integral_constant<int, 1>{});
+            step(std::integral_constant<int, 2>{});
+            step(std::integral_constant<int, 3>{});
+        }
+
+        // ---- lane l holds row l % 32 of a fragment, outputs 8 g + 4 (l / 32) + 0..3 in
+        // registers 4 g ..
+        int tm, tn;
+        tile_at(ck, tm, tn);
+        const int64_t m0 = (int64_t)tm * BM + wm * 32 * FM;
+        const int n0 = tn * BN + wn * 32 * FO;
+        uint8_t *stage = smem + 2 * STAGE + wave * OUT_WAVE;
+#pragma unroll
+        for (int j = 0; j < FM; ++j) {
+#pragma unroll
+            for (int f0 = 0; f0 < FO; f0 += EW) {
+                if constexpr (EPI == kGatedQuant) {
+#pragma unroll
+                    for (int e = 0; e < EW; ++e) {
+                        float v[16];
+#pragma unroll
+                        for (int x = 0; x < 16; ++x) v[x] = silu(acc[f0 + e][j][x]) * acc[f0 + e + FO][j][x];
+                        uint32_t byte;
+                        const uint2 c = mx4_quantize_halves(v, byte);
+                        const int64_t m = m0 + 32 * j + r;
+                        const int n = n0 + 32 * (f0 + e);
+                        if (m < p.M && n < p.N) {
+                            reinterpret_cast<uint2 *>(p.codes)[(m * p.N + n) / 16 + h] = c;
+                            if (h == 0) p.scales[m * p.out_stride + n / 32] = (uint8_t)byte;
+                        }
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < EW; ++e)
+#pragma unroll
+                        for (int g = 0; g < 4; ++g) {
+                            float o[4];
+#pragma unroll
+                            for (int x = 0; x < 4; ++x) {
+                                o[x] = acc[f0 + e][j][4 * g + x];
+                                if constexpr (EPI == kGated) o[x] = silu(o[x]) * acc[(f0 + e + FO) % FN][j][4 * g + x];
+                            }
+                            const int chunk = (4 * e + g) ^ (r & (4 * EW - 1));
+                            *reinterpret_cast<uint2 *>(stage + r * OUT_ROW + chunk * 16 + 8 * h) =
+                                make_uint2(round16x2<BF16>(o[0], o[1]), round16x2<BF16>(o[2], o[3]));
+                        }
+                    constexpr int LR = 4 * EW;             // lanes per row
+#pragma unroll
+                    for (int s = 0; s < 32 / (64 / LR); ++s) {
+                        const int row = s * (64 / LR) + lane / LR, c = lane % LR;
+                        const uint4 val = *reinterpret_cast<const uint4 *>(stage + row * OUT_ROW + ((c ^ (row & (LR - 1))) << 4));
+                        const int64_t m = m0 + 32 * j + row;
+                        const int n = n0 + 32 * f0 + 8 * c;
+                        store8(p, m, n, val);
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        if constexpr (EPI == kGatedQuant) {
+            // the padding behind a row's last block
+            const int64_t m = (int64_t)tm * BM + threadIdx.x;
+            if (tn == tiles_n - 1 && (int)threadIdx.x < BM && m < p.M)
+                for (int64_t i = p.N / 32; i < p.out_stride; ++i) p.scales[m * p.out_stride + i] = 0;
+        }
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // no DMA into LDS past the end
+}
+
+template <int EPI, bool BF16, int FM, int FN>
+hipError_t launch_tile(const Mx4Product &p, hipStream_t stream) {
+    constexpr int BM = 64 * FM, BN = (EPI == kLinear ? 64 : 32) * FN;
+    const int tiles_m = (int)(((int64_t)p.M + BM - 1) / BM), tiles_n = (p.N + BN - 1) / BN;
+    const int64_t T = (int64_t)tiles_m * tiles_n;
+    const int64_t grid = std::min<int64_t>(T, (int64_t)device_cus() * (FM * FN >= 16 ? 1 : 2));
+    hipLaunchKernelGGL((k_mx4_tile<EPI, BF16, FM, FN>), dim3((unsigned)grid), dim3(256), 0, stream, p, tiles_m, tiles_n);
+    return hipGetLastError();
+}
+
 template <int EPI, bool BF16>
 hipError_t launch_typed(const Mx4Product &p, hipStream_t stream) {
+    if (p.M > 64) {
+        const int64_t tiles = (((int64_t)p.M + 255) / 256) * ((p.N + (EPI == kLinear ? 255 : 127)) / (EPI == kLinear ? 256 : 128));
+        return tiles >= device_cus() ? launch_tile<EPI, BF16, 4, 4>(p, stream) : launch_tile<EPI, BF16, 2, 2>(p, stream);
+    }
     const dim3 grid((unsigned)((p.N + 31) / 32), (unsigned)(((int64_t)p.M + 31) / 32));
     hipLaunchKernelGGL((k_mx4_skinny<EPI, BF16, 1>), grid, dim3(64 * kSkinnyWaves), 0, stream, p);
     return hipGetLastError();
