@@ -33,7 +33,10 @@ __device__ __forceinline__ void mfma_mx4(v4i w, uint32_t sw, v4i a, uint32_t sa,
     acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(W, A, acc, 4, 4, I, (int)sw, I, (int)sa);
 }
 
-__device__ __forceinline__ float silu(float g) { return g / (1.0f + __expf(-g)); }
+// (the hardware's exp2 and reciprocal, one unit in the last place each)
+__device__ __forceinline__ float silu(float g) {
+    return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896341f * g));
+}
 
 // 8 consecutive 16-bit outputs n0 .. n0 + 7 of row m, as far as they exist
 __device__ __forceinline__ void store8(const Mx4Product &p, int64_t m, int n0, uint4 w) {
@@ -184,18 +187,25 @@ __global__ __launch_bounds__(64 * kSkinnyWaves) void k_mx4_skinny(const Mx4Produ
 // ---- tiles through LDS -----------------------------------------------------------
 // A work-group of four wavefronts, 2 x 2, computes 64 FM rows by 64 FN weight
 // rows, each wavefront FM x FN fragments of 32 x 32.  k runs in stages of 256
-// values; a ring of two stages in LDS is filled by DMA and runs on across the
-// tiles of a persistent work-group.
-//  * A stage's row is 128 bytes, one cache line, loaded by 8 lanes.  Chunk c of
-//    16 bytes (32 codes) of row r lies at c ^ (r % 8), so that the 32 rows of a
-//    fragment read fall into distinct banks.
-//  * The operands of a 64-value step are read while the step before it is
-//    multiplied.  The last step of a stage waits for the next stage's DMA and for
-//    every wavefront to hold this one's last operands; from there the slot takes
-//    the stage after the next.
+// values, four steps each; two stages fit in LDS, filled by DMA, and the ring
+// runs on across the tiles of a persistent work-group.
+//  * A stage's row is 128 bytes, one cache line, loaded by 8 lanes: what the DMA
+//    costs is lines touched per instruction, and rows of half a line cost a third
+//    more time.  Chunk c of 16 bytes (32 codes) of row r lies at c ^ (r / 2 % 8),
+//    so that 16 rows of a fragment read fall into distinct banks.
+//  * Scale bytes come 16 per row, for two stages at once: the rows of a with the
+//    odd stage before, those of w with the even one.  An odd number of stages is
+//    padded with one that multiplies nothing.
+//  * Operands are read ahead of their step: during steps 2 and 3 those of the next
+//    stage's steps 0 to 2, during step 0 those of step 3.  So a slot is read in
+//    three steps and has five for its next stage to arrive, whose DMAs are spread
+//    over the products of steps 1 to 3.
 //  * Past the row's end the DMA's offsets lie outside the buffer and give codes
 //    of zero, and the scale bytes there are masked; rows past the last are outside
 //    it too.
+// No instruction: x is taken to change here.
+__device__ __forceinline__ void hold(v16f &x) { asm volatile("" : "+a"(x)); }
+
 template <class F, int... I>
 __device__ __forceinline__ void unrolled_seq(F &&f, std::integer_sequence<int, I...>) {
     (f(std::integral_constant<int, I>{}), ...);
@@ -207,26 +217,27 @@ __device__ __forceinline__ void unrolled(F &&f) {
 }
 
 constexpr int kRowBytes = 128;                   // codes of a row in a stage
-constexpr int kRowScales = 8;
+constexpr int kRowScales = 16;                   // scale bytes of a row, two stages'
 
 template <int EPI, bool BF16, int FM, int FN>
 __global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void k_mx4_tile(const Mx4Product p, int tiles_m, int tiles_n) {
     constexpr int BM = 64 * FM, BW = 64 * FN;              // rows of a, of w
     constexpr int BN = EPI == kLinear ? BW : BW / 2;       // outputs: half of w's rows are the gate's
     constexpr int FO = EPI == kLinear ? FN : FN / 2;       // fragments of outputs per wavefront
-    constexpr int OFF_W = BM * kRowBytes, OFF_SA = OFF_W + BW * kRowBytes, OFF_SW = OFF_SA + BM * kRowScales;
-    constexpr int STAGE = OFF_SW + BW * kRowScales;
-    constexpr int EW = FO >= 2 && FM * FN >= 16 ? 2 : 1;                    // fragments stored together
+    constexpr int OFF_W = BM * kRowBytes, STAGE = OFF_W + BW * kRowBytes;
+    constexpr int OFF_SCALES = 2 * STAGE, OFF_SW = BM * kRowScales, SCALES = OFF_SW + BW * kRowScales;
+    constexpr int OFF_OUT = OFF_SCALES + 2 * SCALES;
+    constexpr int EW = FO >= 2 && FM * FN >= 16 ? 2 : 1;   // fragments stored together
     constexpr int OUT_ROW = 64 * EW, OUT_WAVE = EPI == kGatedQuant ? 0 : 32 * OUT_ROW;
-    constexpr int CODE_DMAS = 2 * (FM + FN), SCALE_DMAS = (FM + FN) / 2, DMAS = CODE_DMAS + SCALE_DMAS;
+    constexpr int CODE_DMAS = 2 * (FM + FN), DMAS = CODE_DMAS + 1;
     static_assert(EPI == kLinear || FN % 2 == 0, "gate and up fragments");
-    static_assert((FM + FN) % 2 == 0, "scale loads");
-    __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * STAGE + 4 * OUT_WAVE];
+    static_assert(FM <= 4 && FN <= 4, "a wavefront's share of the scales is one load");
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[OFF_OUT + 4 * OUT_WAVE];
 
     const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int wm = wave & 1, wn = wave >> 1;
-    const int blocks = p.K / 32, KT = (blocks + 7) / 8;
+    const int blocks = p.K / 32, KT = (blocks + 7) / 8, KT2 = (KT + 1) & ~1;
     const uint32_t kb = (uint32_t)p.K / 2, sb = (uint32_t)p.in_stride;
 
     // this work-group's tiles: a contiguous share of its XCD's range
@@ -242,60 +253,88 @@ __global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void k_mx4_tile(const M
         grouped_tile(start + i0 + k * nb, tiles_m, tiles_n, tm, tn);
     };
 
-    // ---- DMA: one stage is issue_begin(), then issue(i) for i < DMAS
+    // ---- DMA.  A stage is issue_begin(), then issue(i) for i < DMAS: its codes and
+    // a quarter per wavefront of the scales of w (even stages, for themselves and the
+    // next) or of a (odd ones, for the two stages behind them).  Buffers of the tile
+    // of the codes; those of a's scales are a stage ahead.
     const uint32_t lds = lds_addr(smem);
-    const uint32_t c_row = (uint32_t)lane >> 3, c_chunk = ((uint32_t)lane & 7u) ^ c_row;
-    const uint32_t v_codes = c_row * kb + c_chunk * 16u;
-    const uint32_t v_scales = ((uint32_t)lane >> 1) * sb + ((uint32_t)lane & 1u) * 4u;
+    const uint32_t c_row = (uint32_t)lane >> 3;
+    const uint32_t c_chunk[2] = {((uint32_t)lane & 7u) ^ (c_row >> 1), ((uint32_t)lane & 7u) ^ (c_row >> 1) ^ 4u};
     constexpr uint32_t kOutside = 0x80000000u;
-    int iss_tile = -1, iss_kt = KT - 1, iss_slot = 1;
-    v4i dA = {}, dW = {}, dSA = {}, dSG = {}, dSU = {};
-    uint32_t iss_v = 0, iss_s = 0, iss_lds = 0;
+    int iss_tile = -1, iss_kt = KT2 - 1, iss_slot = 1, sc_tile = -1, sc_kt = KT2 - 2, sc_slot = 1;
+    v4i dA = {}, dW = {}, dSA = {}, dSW = {};
+    uint32_t iss_v[2] = {}, iss_lds = 0;
+    auto rows_of = [](int64_t total, int64_t first, int most) __attribute__((always_inline)) {
+        return (uint32_t)min(total - first, (int64_t)most);
+    };
+    // the place of the next two stages' scales of a
+    auto scales_a = [&]() __attribute__((always_inline)) {
+        sc_kt += 2;
+        sc_slot ^= 1;
+        if (sc_kt == KT2) {
+            sc_kt = 0;
+            ++sc_tile;
+            int tm = 0, tn = 0;
+            if (sc_tile < nt) tile_at(sc_tile, tm, tn);
+            const int64_t m0 = (int64_t)tm * BM;
+            dSA = buffer_desc(p.as + m0 * sb, sc_tile < nt ? rows_of(p.M, m0, BM) * sb : 0u);
+        }
+    };
     auto issue_begin = [&]() __attribute__((always_inline)) {
-        if (++iss_kt == KT) {
+        if (++iss_kt == KT2) {
             iss_kt = 0;
             ++iss_tile;
             const bool live = iss_tile < nt;               // past the last tile: empty buffers
             int tm = 0, tn = 0;
             if (live) tile_at(iss_tile, tm, tn);
             const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
-            const uint32_t ra = live ? (uint32_t)min((int64_t)p.M - m0, (int64_t)BM) : 0u;
-            const uint32_t rw = live ? (uint32_t)min((int64_t)p.N - n0, (int64_t)BN) : 0u;
-            const int64_t up = EPI == kLinear ? 0 : p.N;   // the up rows' distance
-            dA = buffer_desc(p.a + m0 * kb, ra * kb);
-            dSA = buffer_desc(p.as + m0 * sb, ra * sb);
-            dW = buffer_desc(p.w + (n0 + (wave >= 2 ? up : 0)) * kb, rw * kb);
-            dSG = buffer_desc(p.ws + n0 * sb, rw * sb);
-            dSU = buffer_desc(p.ws + (n0 + up) * sb, rw * sb);
+            // wavefronts 2 and 3 load the second half of w's rows: the up rows
+            const int64_t w0 = n0 + (EPI != kLinear && wave >= 2 ? (int64_t)p.N : 0);
+            const uint32_t rw = live ? rows_of(p.N, n0, BN) : 0u;
+            dA = buffer_desc(p.a + m0 * kb, live ? rows_of(p.M, m0, BM) * kb : 0u);
+            dW = buffer_desc(p.w + w0 * kb, rw * kb);
+            dSW = buffer_desc(p.ws + w0 * sb, rw * sb);
         }
+        if (iss_kt & 1) scales_a();
         iss_slot ^= 1;
         iss_lds = lds + (uint32_t)iss_slot * STAGE;
-        iss_v = (uint32_t)iss_kt * 8u + c_chunk < (uint32_t)blocks ? v_codes + (uint32_t)iss_kt * kRowBytes : kOutside;
-        iss_s = v_scales + (uint32_t)iss_kt * kRowScales;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const uint32_t c = (uint32_t)iss_kt * 8u + c_chunk[x];
+            iss_v[x] = c < (uint32_t)blocks ? c_row * kb + c * 16u : kOutside;
+        }
     };
     auto issue = [&](auto i_c) __attribute__((always_inline)) {
         constexpr int i = decltype(i_c)::value;
-        if constexpr (i < 2 * FM) {                        // 8 rows of a
-            const uint32_t g = (uint32_t)(wave * 2 * FM + i);
-            dma16(dA, iss_v + g * 8u * kb, iss_lds + g * 1024u);
-        } else if constexpr (i < CODE_DMAS) {              // 8 rows of w; wavefronts 2 and 3: the second half
-            const uint32_t g = (uint32_t)(wave * 2 * FN + i - 2 * FM);
-            const uint32_t row = EPI == kLinear ? g : (uint32_t)((wave & 1) * 2 * FN + i - 2 * FM);
-            dma16(dW, iss_v + row * 8u * kb, iss_lds + OFF_W + g * 1024u);
-        } else {                                           // the scales of 32 rows of a or w
-            const uint32_t g = (uint32_t)(wave * SCALE_DMAS + i - CODE_DMAS);
-            if (g < 2 * FM) {
-                dma4(dSA, iss_s + g * 32u * sb, iss_lds + OFF_SA + g * 256u);
+        if constexpr (i == 0) {
+            const uint32_t base = lds + OFF_SCALES + (uint32_t)sc_slot * SCALES;
+            if (iss_kt & 1) {
+                const uint32_t row = (uint32_t)wave * 16 * FM;
+                if (lane < 16 * FM)
+                    dma16(dSA, (row + (uint32_t)lane) * sb + (uint32_t)sc_kt * 8u, base + row * kRowScales);
             } else {
-                const uint32_t w = g - 2 * FM;
-                const bool second = EPI != kLinear && w >= FN;
-                dma4(second ? dSU : dSG, iss_s + (second ? w - FN : w) * 32u * sb, iss_lds + OFF_SW + w * 256u);
+                const uint32_t row = (uint32_t)wave * 16 * FN;
+                const uint32_t from = EPI == kLinear ? row : (uint32_t)(wave & 1) * 16 * FN;
+                if (lane < 16 * FN)
+                    dma16(dSW, (from + (uint32_t)lane) * sb + (uint32_t)iss_kt * 8u, base + OFF_SW + row * kRowScales);
             }
+        } else if constexpr (i <= 2 * FM) {                // 8 rows of a
+            const uint32_t g = (uint32_t)(wave * 2 * FM + i - 1);
+            dma16(dA, iss_v[(i - 1) & 1] + g * 8u * kb, iss_lds + g * 1024u);
+        } else {                                           // 8 rows of w
+            constexpr int j = i - 1 - 2 * FM;
+            const uint32_t g = (uint32_t)(wave * 2 * FN + j);
+            const uint32_t row = EPI == kLinear ? g : (uint32_t)((wave & 1) * 2 * FN + j);
+            dma16(dW, iss_v[j & 1] + row * 8u * kb, iss_lds + OFF_W + g * 1024u);
         }
     };
-    auto issue_all = [&]() __attribute__((always_inline)) {
-        issue_begin();
-        unrolled<DMAS>(issue);
+    // Part x of the stage's DMAs, of `of` parts
+    auto issue_part = [&](auto x_c, auto of_c) __attribute__((always_inline)) {
+        constexpr int x = decltype(x_c)::value, of = decltype(of_c)::value;
+        constexpr int lo = x * DMAS / of, hi = (x + 1) * DMAS / of;
+        unrolled<hi - lo>([&](auto d_c) __attribute__((always_inline)) {
+            issue(std::integral_constant<int, lo + decltype(d_c)::value>{});
+        });
     };
 
     // ---- operands of a step
@@ -304,34 +343,49 @@ __global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void k_mx4_tile(const M
     auto w_row = [&](int f) { return EPI == kLinear || f < FO ? 32 * f : BN + 32 * (f - FO); };
     uint32_t xo[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) xo[i] = (uint32_t)(r * kRowBytes + (((4 * h + i) ^ (r & 7)) << 4));
+    for (int i = 0; i < 4; ++i) xo[i] = (uint32_t)(r * kRowBytes + (((4 * h + i) ^ ((r >> 1) & 7)) << 4));
     const uint32_t a_at = (uint32_t)(wm * 32 * FM * kRowBytes), w_at = (uint32_t)(OFF_W + row_w * kRowBytes);
-    const uint32_t sa_at = (uint32_t)(OFF_SA + (wm * 32 * FM + r) * kRowScales + 4 * h);
-    const uint32_t sw_at = (uint32_t)(OFF_SW + (row_w + r) * kRowScales + 4 * h);
-    v4i a[2][FM], w[2][FN];
+    const uint32_t sa_at = (uint32_t)(OFF_SCALES + (wm * 32 * FM + r) * kRowScales + 4 * h);
+    const uint32_t sw_at = (uint32_t)(OFF_SCALES + OFF_SW + (row_w + r) * kRowScales + 4 * h);
+    v4i a[4][FM], w[4][FN];
     uint32_t ra[FM], rw[FN], sa[FM], sw[FN];
-    auto read_step = [&](uint32_t slot, auto i_c, auto set_c) __attribute__((always_inline)) {
-        constexpr int i = decltype(i_c)::value, S = decltype(set_c)::value;
+    auto read_step = [&](uint32_t slot, auto i_c) __attribute__((always_inline)) {
+        constexpr int i = decltype(i_c)::value;
         const uint8_t *b = smem + slot * STAGE + xo[i];
 #pragma unroll
-        for (int j = 0; j < FM; ++j) a[S][j] = *reinterpret_cast<const v4i *>(b + a_at + 32 * kRowBytes * j);
+        for (int j = 0; j < FM; ++j) a[i][j] = *reinterpret_cast<const v4i *>(b + a_at + 32 * kRowBytes * j);
 #pragma unroll
-        for (int f = 0; f < FN; ++f) w[S][f] = *reinterpret_cast<const v4i *>(b + w_at + kRowBytes * w_row(f));
+        for (int f = 0; f < FN; ++f) w[i][f] = *reinterpret_cast<const v4i *>(b + w_at + kRowBytes * w_row(f));
     };
-    auto read_scales = [&](uint32_t slot) __attribute__((always_inline)) {
-        const uint8_t *b = smem + slot * STAGE;
+    auto read_scales = [&](uint32_t slot, uint32_t half) __attribute__((always_inline)) {
+        const uint8_t *b = smem + slot * SCALES + half * 8;
 #pragma unroll
         for (int j = 0; j < FM; ++j) ra[j] = *reinterpret_cast<const uint32_t *>(b + sa_at + 32 * kRowScales * j);
 #pragma unroll
         for (int f = 0; f < FN; ++f) rw[f] = *reinterpret_cast<const uint32_t *>(b + sw_at + kRowScales * w_row(f));
     };
+    typedef std::integral_constant<int, 0> c0;
+    typedef std::integral_constant<int, 1> c1;
+    typedef std::integral_constant<int, 2> c2;
+    typedef std::integral_constant<int, 3> c3;
 
-    issue_all();
-    issue_all();
+    // the first stage's scales of a, then what two stages before the first would have issued
+    constexpr int PARTS = 3 * FM * FN, EARLY = FM * FN * DMAS / PARTS;
+    scales_a();
+    if (lane < 16 * FM) {
+        const uint32_t row = (uint32_t)wave * 16 * FM;
+        dma16(dSA, (row + (uint32_t)lane) * sb, lds + OFF_SCALES + (uint32_t)sc_slot * SCALES + row * kRowScales);
+    }
+    issue_begin();
+    unrolled<DMAS>(issue);
+    issue_begin();
+    unrolled<DMAS>(issue);
     asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(DMAS) : "memory");
-    uint32_t slot = 0;
-    read_step(0, std::integral_constant<int, 0>{}, std::integral_constant<int, 0>{});
-    read_scales(0);
+    uint32_t slot = 0, s_slot = 0;                         // of the stage that is read next
+    read_step(0, c0{});
+    read_scales(0, 0);
+    read_step(0, c1{});
+    read_step(0, c2{});
 
     for (int ck = 0; ck < nt; ++ck) {
         v16f acc[FN][FM];
@@ -339,7 +393,9 @@ __global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void k_mx4_tile(const M
         for (int f = 0; f < FN; ++f)
 #pragma unroll
             for (int j = 0; j < FM; ++j) acc[f][j] = v16f{};
-        for (int kt = 0; kt < KT; ++kt) {
+        // One stage; not LIVE: one that pads their number to an even one
+        auto stage = [&](int kt, auto live_c) __attribute__((always_inline)) {
+            constexpr bool LIVE = decltype(live_c)::value;
             const int left = blocks - 8 * kt - 4 * h;
             const uint32_t mask = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
 #pragma unroll
@@ -347,35 +403,43 @@ __global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void k_mx4_tile(const M
 #pragma unroll
             for (int f = 0; f < FN; ++f) sw[f] = rw[f] & mask;
             auto step = [&](auto i_c) __attribute__((always_inline)) {
-                constexpr int i = decltype(i_c)::value, S = i & 1;
-                if constexpr (i < 3) {
-                    read_step(slot, std::integral_constant<int, i + 1>{}, std::integral_constant<int, 1 - S>{});
-                } else {
-                    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-                    slot ^= 1;
+                constexpr int i = decltype(i_c)::value;
+                if constexpr (i == 0) read_step(slot, c3{});
+                if constexpr (i == 1) {
+                    // every wavefront holds this stage's operands: its slot is free
+                    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
                     issue_begin();
-                    read_step(slot, std::integral_constant<int, 0>{}, std::integral_constant<int, 0>{});
-                    read_scales(slot);
+                }
+                if constexpr (i == 2) {
+                    // the next stage has landed (in order: only what step 1 issued may be outstanding)
+                    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(EARLY) : "memory");
+                    slot ^= 1;
+                    if (kt & 1) s_slot ^= 1;
+                    read_step(slot, c0{});
+                    read_scales(s_slot, (uint32_t)(kt + 1) & 1u);
+                }
+                if constexpr (i == 3) {
+                    read_step(slot, c1{});
+                    read_step(slot, c2{});
                 }
                 __builtin_amdgcn_sched_barrier(0);
                 unrolled<FM * FN>([&](auto x_c) __attribute__((always_inline)) {
                     constexpr int x = decltype(x_c)::value, f = x / FM, j = x % FM;
-                    mfma_mx4<i>(w[S][f], sw[f], a[S][j], sa[j], acc[f][j]);
-                    if constexpr (i == 3) {                // the DMAs spread over the step's products
-                        constexpr int lo = x * DMAS / (FM * FN), hi = (x + 1) * DMAS / (FM * FN);
-                        unrolled<hi - lo>([&](auto d_c) __attribute__((always_inline)) {
-                            issue(std::integral_constant<int, lo + decltype(d_c)::value>{});
-                        });
+                    if constexpr (LIVE) mfma_mx4<i>(w[i][f], sw[f], a[i][j], sa[j], acc[f][j]);
+                    if constexpr (i > 0) {
+                        issue_part(std::integral_constant<int, (i - 1) * FM * FN + x>{}, std::integral_constant<int, PARTS>{});
                         __builtin_amdgcn_sched_barrier(0);
                     }
                 });
                 __builtin_amdgcn_sched_barrier(0);
             };
-            step(std::integral_constant<int, 0>{});
-            step(std::integral_constant<int, 1>{});
-            step(std::integral_constant<int, 2>{});
-            step(std::integral_constant<int, 3>{});
-        }
+            step(c0{});
+            step(c1{});
+            step(c2{});
+            step(c3{});
+        };
+        for (int kt = 0; kt < KT; ++kt) stage(kt, std::true_type{});
+        if (KT2 != KT) stage(KT, std::false_type{});
 
         // ---- lane l holds row l % 32 of a fragment, outputs 8 g + 4 (l / 32) + 0..3 in
         // registers 4 g ..
@@ -383,11 +447,17 @@ __global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void k_mx4_tile(const M
         tile_at(ck, tm, tn);
         const int64_t m0 = (int64_t)tm * BM + wm * 32 * FM;
         const int n0 = tn * BN + wn * 32 * FO;
-        uint8_t *stage = smem + 2 * STAGE + wave * OUT_WAVE;
+        uint8_t *out = smem + OFF_OUT + wave * OUT_WAVE;
 #pragma unroll
         for (int j = 0; j < FM; ++j) {
 #pragma unroll
             for (int f0 = 0; f0 < FO; f0 += EW) {
+                // (opaque here, so that no later pass's sums are read before their turn)
+#pragma unroll
+                for (int e = 0; e < EW; ++e) {
+                    hold(acc[f0 + e][j]);
+                    if constexpr (EPI != kLinear) hold(acc[f0 + e + FO][j]);
+                }
                 if constexpr (EPI == kGatedQuant) {
 #pragma unroll
                     for (int e = 0; e < EW; ++e) {
@@ -415,14 +485,14 @@ __global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void k_mx4_tile(const M
                                 if constexpr (EPI == kGated) o[x] = silu(o[x]) * acc[(f0 + e + FO) % FN][j][4 * g + x];
                             }
                             const int chunk = (4 * e + g) ^ (r & (4 * EW - 1));
-                            *reinterpret_cast<uint2 *>(stage + r * OUT_ROW + chunk * 16 + 8 * h) =
+                            *reinterpret_cast<uint2 *>(out + r * OUT_ROW + chunk * 16 + 8 * h) =
                                 make_uint2(round16x2<BF16>(o[0], o[1]), round16x2<BF16>(o[2], o[3]));
                         }
                     constexpr int LR = 4 * EW;             // lanes per row
 #pragma unroll
                     for (int s = 0; s < 32 / (64 / LR); ++s) {
                         const int row = s * (64 / LR) + lane / LR, c = lane % LR;
-                        const uint4 val = *reinterpret_cast<const uint4 *>(stage + row * OUT_ROW + ((c ^ (row & (LR - 1))) << 4));
+                        const uint4 val = *reinterpret_cast<const uint4 *>(out + row * OUT_ROW + ((c ^ (row & (LR - 1))) << 4));
                         const int64_t m = m0 + 32 * j + row;
                         const int n = n0 + 32 * f0 + 8 * c;
                         store8(p, m, n, val);

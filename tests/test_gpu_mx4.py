@@ -214,7 +214,8 @@ def fp32_sums(K):
 
 SIZES = [(1, 1, 32), (1, 33, 64), (3, 5, 96), (16, 32, 256), (17, 31, 288), (31, 65, 480), (32, 64, 512), (33, 100, 1056),
          (64, 256, 4096), (65, 129, 544), (128, 128, 1024), (130, 257, 1120), (257, 300, 320), (300, 520, 1568),
-         (1, 4096, 4096), (5, 1000, 5120), (513, 768, 768), (1025, 1031, 1056), (2049, 2080, 512)]
+         (1, 4096, 4096), (5, 1000, 5120), (513, 768, 768), (1025, 1031, 1056), (2049, 2080, 512),
+         (4100, 4200, 96), (3000, 6200, 1184), (16400, 1030, 288)]
 
 
 @pytest.mark.parametrize("M,N,K", SIZES)
@@ -243,7 +244,7 @@ def test_linear_rounding(M, N, K):
     check_product(p4q.mx4_linear(*gpu(a), *gpu(b)), ref, mag, K, "bf16")
 
 
-@pytest.mark.parametrize("M", [3, 40, 600])
+@pytest.mark.parametrize("M", [3, 40, 600, 66000])
 def test_linear_row_gaps(M):
     N, K = 200, 288
     a, w = exact_operands(3, M, N, K)
@@ -255,7 +256,7 @@ def test_linear_row_gaps(M):
         assert bool((wide[:, :first] == 7).all()) and bool((wide[:, first + N:] == 7).all())
 
 
-@pytest.mark.parametrize("M", [2, 50, 400])
+@pytest.mark.parametrize("M", [2, 50, 400, 66000])
 def test_linear_nan_and_extreme_scales(M):
     N, K = 130, 608
     a, w = exact_operands(4, M, N, K)
@@ -289,7 +290,8 @@ def gated_reference(a, w, N, K, exact):
 
 
 GATED = [(1, 32, 32), (1, 33, 64), (7, 1, 96), (16, 64, 1056), (33, 100, 288), (40, 352, 4096), (130, 129, 320), (300, 260, 544),
-         (520, 512, 512), (1030, 1056, 288), (2050, 1030, 256)]
+         (520, 512, 512), (1030, 1056, 288), (2050, 1030, 256),
+         (4100, 2112, 96), (2900, 3011, 544)]
 
 
 @pytest.mark.parametrize("M,N,K", GATED)
