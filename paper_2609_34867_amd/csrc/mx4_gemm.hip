@@ -42,8 +42,8 @@ __device__ __forceinline__ float silu(float g) {
 __device__ __forceinline__ void store8(const Mx4Product &p, int64_t m, int n0, uint4 w) {
     if (m >= p.M || n0 >= p.N) return;
     uint16_t *dst = static_cast<uint16_t *>(p.y) + m * p.ldy + n0;
-    if (p.wide && n0 + 8 <= p.N) {
-        *reinterpret_cast<uint4 *>(dst) = w;
+    if (n0 + 8 <= p.N) {
+        __builtin_memcpy(dst, &w, 16);                     // one store, whatever the row's alignment
     } else {
         const uint32_t x[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
@@ -387,15 +387,14 @@ __global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void k_mx4_tile(const M
     read_step(0, c1{});
     read_step(0, c2{});
 
+    constexpr int STORES = EPI == kGatedQuant ? 0 : FM * FO / EW * (32 * 4 * EW / 64);
+    bool stored = false;
     for (int ck = 0; ck < nt; ++ck) {
         v16f acc[FN][FM];
-#pragma unroll
-        for (int f = 0; f < FN; ++f)
-#pragma unroll
-            for (int j = 0; j < FM; ++j) acc[f][j] = v16f{};
-        // One stage; not LIVE: one that pads their number to an even one
-        auto stage = [&](int kt, auto live_c) __attribute__((always_inline)) {
-            constexpr bool LIVE = decltype(live_c)::value;
+        // One stage: the first, whose sums begin, one between, or one that pads their
+        // number to an even one
+        auto stage = [&](int kt, auto kind_c) __attribute__((always_inline)) {
+            constexpr bool FIRST = decltype(kind_c)::value == 0, LIVE = decltype(kind_c)::value < 2;
             const int left = blocks - 8 * kt - 4 * h;
             const uint32_t mask = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
 #pragma unroll
@@ -411,8 +410,11 @@ __global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void k_mx4_tile(const M
                     issue_begin();
                 }
                 if constexpr (i == 2) {
-                    // the next stage has landed (in order: only what step 1 issued may be outstanding)
-                    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(EARLY) : "memory");
+                    // the next stage has landed (in order: what step 1 issued may be outstanding,
+                    // and the stores of the tile before)
+                    if (FIRST && stored) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(EARLY + STORES) : "memory");
+                    else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(EARLY) : "memory");
+                    asm volatile("s_barrier" ::: "memory");
                     slot ^= 1;
                     if (kt & 1) s_slot ^= 1;
                     read_step(slot, c0{});
@@ -425,6 +427,7 @@ __global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void k_mx4_tile(const M
                 __builtin_amdgcn_sched_barrier(0);
                 unrolled<FM * FN>([&](auto x_c) __attribute__((always_inline)) {
                     constexpr int x = decltype(x_c)::value, f = x / FM, j = x % FM;
+                    if constexpr (FIRST && i == 0) acc[f][j] = v16f{};
                     if constexpr (LIVE) mfma_mx4<i>(w[i][f], sw[f], a[i][j], sa[j], acc[f][j]);
                     if constexpr (i > 0) {
                         issue_part(std::integral_constant<int, (i - 1) * FM * FN + x>{}, std::integral_constant<int, PARTS>{});
@@ -438,8 +441,9 @@ __global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void k_mx4_tile(const M
             step(c2{});
             step(c3{});
         };
-        for (int kt = 0; kt < KT; ++kt) stage(kt, std::true_type{});
-        if (KT2 != KT) stage(KT, std::false_type{});
+        stage(0, c0{});
+        for (int kt = 1; kt < KT; ++kt) stage(kt, c1{});
+        if (KT2 != KT) stage(KT, c2{});
 
         // ---- lane l holds row l % 32 of a fragment, outputs 8 g + 4 (l / 32) + 0..3 in
         // registers 4 g ..
@@ -447,6 +451,9 @@ __global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void k_mx4_tile(const M
         tile_at(ck, tm, tn);
         const int64_t m0 = (int64_t)tm * BM + wm * 32 * FM;
         const int n0 = tn * BN + wn * 32 * FO;
+        // (its stores, counted for the next tile's first wait)
+        const bool full = (int64_t)(tm + 1) * BM <= p.M && (int64_t)(tn + 1) * BN <= p.N;
+        stored = full && EPI != kGatedQuant;
         uint8_t *out = smem + OFF_OUT + wave * OUT_WAVE;
 #pragma unroll
         for (int j = 0; j < FM; ++j) {
@@ -495,7 +502,8 @@ __global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void k_mx4_tile(const M
                         const uint4 val = *reinterpret_cast<const uint4 *>(out + row * OUT_ROW + ((c ^ (row & (LR - 1))) << 4));
                         const int64_t m = m0 + 32 * j + row;
                         const int n = n0 + 32 * f0 + 8 * c;
-                        store8(p, m, n, val);
+                        if (full) __builtin_memcpy(static_cast<uint16_t *>(p.y) + m * p.ldy + n, &val, 16);
+                        else store8(p, m, n, val);
                     }
                 }
                 __builtin_amdgcn_sched_barrier(0);
@@ -536,7 +544,6 @@ hipError_t launch_typed(const Mx4Product &p, hipStream_t stream) {
 
 hipError_t launch_mx4_linear(p4q_dtype out_dt, Mx4Product p, hipStream_t stream) {
     p.in_stride = mx4_scale_stride(p.K);
-    p.wide = p.ldy % 8 == 0 && reinterpret_cast<uintptr_t>(p.y) % 16 == 0;
     return out_dt == P4Q_BF16 ? launch_typed<kLinear, true>(p, stream) : launch_typed<kLinear, false>(p, stream);
 }
 
@@ -544,7 +551,6 @@ hipError_t launch_mx4_gated(p4q_dtype out_dt, Mx4Product p, hipStream_t stream) 
     p.in_stride = mx4_scale_stride(p.K);
     p.out_stride = mx4_scale_stride(p.N);
     if (p.codes) return launch_typed<kGatedQuant, false>(p, stream);
-    p.wide = p.ldy % 8 == 0 && reinterpret_cast<uintptr_t>(p.y) % 16 == 0;
     return out_dt == P4Q_BF16 ? launch_typed<kGated, true>(p, stream) : launch_typed<kGated, false>(p, stream);
 }
 
