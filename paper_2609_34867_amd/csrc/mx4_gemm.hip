@@ -199,7 +199,8 @@ __global__ __launch_bounds__(64 * kSkinnyWaves) void k_mx4_skinny(const Mx4Produ
 //  * Operands are read ahead of their step: during steps 2 and 3 those of the next
 //    stage's steps 0 to 2, during step 0 those of step 3.  So a slot is read in
 //    three steps and has five for its next stage to arrive, whose DMAs are spread
-//    over the products of steps 1 to 3.
+//    over the products of steps 1 to 3 (over four steps, with less time to arrive,
+//    2% slower).
 //  * Past the row's end the DMA's offsets lie outside the buffer and give codes
 //    of zero, and the scale bytes there are masked; rows past the last are outside
 //    it too.
@@ -349,20 +350,18 @@ __global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void k_mx4_tile(const M
     const uint32_t sw_at = (uint32_t)(OFF_SCALES + OFF_SW + (row_w + r) * kRowScales + 4 * h);
     v4i a[4][FM], w[4][FN];
     uint32_t ra[FM], rw[FN], sa[FM], sw[FN];
-    auto read_step = [&](uint32_t slot, auto i_c) __attribute__((always_inline)) {
-        constexpr int i = decltype(i_c)::value;
+    constexpr int F = FM + FN;
+    auto read_one = [&](uint32_t slot, auto i_c, auto k_c) __attribute__((always_inline)) {
+        constexpr int i = decltype(i_c)::value, k = decltype(k_c)::value;
         const uint8_t *b = smem + slot * STAGE + xo[i];
-#pragma unroll
-        for (int j = 0; j < FM; ++j) a[i][j] = *reinterpret_cast<const v4i *>(b + a_at + 32 * kRowBytes * j);
-#pragma unroll
-        for (int f = 0; f < FN; ++f) w[i][f] = *reinterpret_cast<const v4i *>(b + w_at + kRowBytes * w_row(f));
+        if constexpr (k < FM) a[i][k] = *reinterpret_cast<const v4i *>(b + a_at + 32 * kRowBytes * k);
+        else w[i][k - FM] = *reinterpret_cast<const v4i *>(b + w_at + kRowBytes * w_row(k - FM));
     };
-    auto read_scales = [&](uint32_t slot, uint32_t half) __attribute__((always_inline)) {
+    auto read_scale = [&](uint32_t slot, uint32_t half, auto k_c) __attribute__((always_inline)) {
+        constexpr int k = decltype(k_c)::value;
         const uint8_t *b = smem + slot * SCALES + half * 8;
-#pragma unroll
-        for (int j = 0; j < FM; ++j) ra[j] = *reinterpret_cast<const uint32_t *>(b + sa_at + 32 * kRowScales * j);
-#pragma unroll
-        for (int f = 0; f < FN; ++f) rw[f] = *reinterpret_cast<const uint32_t *>(b + sw_at + kRowScales * w_row(f));
+        if constexpr (k < FM) ra[k] = *reinterpret_cast<const uint32_t *>(b + sa_at + 32 * kRowScales * k);
+        else rw[k - FM] = *reinterpret_cast<const uint32_t *>(b + sw_at + kRowScales * w_row(k - FM));
     };
     typedef std::integral_constant<int, 0> c0;
     typedef std::integral_constant<int, 1> c1;
@@ -370,7 +369,7 @@ __global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void k_mx4_tile(const M
     typedef std::integral_constant<int, 3> c3;
 
     // the first stage's scales of a, then what two stages before the first would have issued
-    constexpr int PARTS = 3 * FM * FN, EARLY = FM * FN * DMAS / PARTS;
+    constexpr int X = FM * FN, PARTS = 3 * X, EARLY = X * DMAS / PARTS;
     scales_a();
     if (lane < 16 * FM) {
         const uint32_t row = (uint32_t)wave * 16 * FM;
@@ -382,13 +381,11 @@ __global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void k_mx4_tile(const M
     unrolled<DMAS>(issue);
     asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(DMAS) : "memory");
     uint32_t slot = 0, s_slot = 0;                         // of the stage that is read next
-    read_step(0, c0{});
-    read_scales(0, 0);
-    read_step(0, c1{});
-    read_step(0, c2{});
+    unrolled<F>([&](auto k) __attribute__((always_inline)) { read_scale(0, 0, k); });
+    unrolled<F>([&](auto k) __attribute__((always_inline)) { read_one(0, c0{}, k); });
+    unrolled<F>([&](auto k) __attribute__((always_inline)) { read_one(0, c1{}, k); });
+    unrolled<F>([&](auto k) __attribute__((always_inline)) { read_one(0, c2{}, k); });
 
-    constexpr int STORES = EPI == kGatedQuant ? 0 : FM * FO / EW * (32 * 4 * EW / 64);
-    bool stored = false;
     for (int ck = 0; ck < nt; ++ck) {
         v16f acc[FN][FM];
         // One stage: the first, whose sums begin, one between, or one that pads their
@@ -403,36 +400,45 @@ __global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void k_mx4_tile(const M
             for (int f = 0; f < FN; ++f) sw[f] = rw[f] & mask;
             auto step = [&](auto i_c) __attribute__((always_inline)) {
                 constexpr int i = decltype(i_c)::value;
-                if constexpr (i == 0) read_step(slot, c3{});
                 if constexpr (i == 1) {
                     // every wavefront holds this stage's operands: its slot is free
                     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
                     issue_begin();
                 }
                 if constexpr (i == 2) {
-                    // the next stage has landed (in order: what step 1 issued may be outstanding,
-                    // and the stores of the tile before)
-                    if (FIRST && stored) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(EARLY + STORES) : "memory");
-                    else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(EARLY) : "memory");
-                    asm volatile("s_barrier" ::: "memory");
+                    // the next stage has landed (in order: only what step 1 issued may be outstanding)
+                    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(EARLY) : "memory");
                     slot ^= 1;
                     if (kt & 1) s_slot ^= 1;
-                    read_step(slot, c0{});
-                    read_scales(s_slot, (uint32_t)(kt + 1) & 1u);
-                }
-                if constexpr (i == 3) {
-                    read_step(slot, c1{});
-                    read_step(slot, c2{});
                 }
                 __builtin_amdgcn_sched_barrier(0);
                 unrolled<FM * FN>([&](auto x_c) __attribute__((always_inline)) {
                     constexpr int x = decltype(x_c)::value, f = x / FM, j = x % FM;
                     if constexpr (FIRST && i == 0) acc[f][j] = v16f{};
                     if constexpr (LIVE) mfma_mx4<i>(w[i][f], sw[f], a[i][j], sa[j], acc[f][j]);
-                    if constexpr (i > 0) {
-                        issue_part(std::integral_constant<int, (i - 1) * FM * FN + x>{}, std::integral_constant<int, PARTS>{});
-                        __builtin_amdgcn_sched_barrier(0);
+                    // behind each product a share of the reads ahead and of the DMAs: a
+                    // wavefront issues in order, and together they would hold up its products
+                    if constexpr (i == 0) {
+                        // (early, for step 1 waits for them)
+                        constexpr int H = X >= 2 ? X / 2 : 1;
+                        constexpr int lo = x < H ? x * F / H : F, hi = x < H ? (x + 1) * F / H : F;
+                        unrolled<hi - lo>([&](auto k) __attribute__((always_inline)) {
+                            read_one(slot, c3{}, std::integral_constant<int, lo + decltype(k)::value>{});
+                        });
                     }
+                    if constexpr (i >= 2) {
+                        constexpr int lo = x * 2 * F / X, hi = (x + 1) * 2 * F / X;
+                        unrolled<hi - lo>([&](auto k_c) __attribute__((always_inline)) {
+                            constexpr int k = lo + decltype(k_c)::value;
+                            typedef std::integral_constant<int, k % F> at;
+                            if constexpr (i == 2 && k < F) read_one(slot, c0{}, at{});
+                            else if constexpr (i == 2) read_scale(s_slot, (uint32_t)(kt + 1) & 1u, at{});
+                            else read_one(slot, std::integral_constant<int, 1 + k / F>{}, at{});
+                        });
+                    }
+                    if constexpr (i > 0)
+                        issue_part(std::integral_constant<int, (i - 1) * X + x>{}, std::integral_constant<int, PARTS>{});
+                    __builtin_amdgcn_sched_barrier(0);
                 });
                 __builtin_amdgcn_sched_barrier(0);
             };
@@ -451,9 +457,7 @@ __global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void k_mx4_tile(const M
         tile_at(ck, tm, tn);
         const int64_t m0 = (int64_t)tm * BM + wm * 32 * FM;
         const int n0 = tn * BN + wn * 32 * FO;
-        // (its stores, counted for the next tile's first wait)
         const bool full = (int64_t)(tm + 1) * BM <= p.M && (int64_t)(tn + 1) * BN <= p.N;
-        stored = full && EPI != kGatedQuant;
         uint8_t *out = smem + OFF_OUT + wave * OUT_WAVE;
 #pragma unroll
         for (int j = 0; j < FM; ++j) {
