@@ -35,6 +35,11 @@ def _ptr(t: Optional[torch.Tensor]):
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
+# (without torch.cuda's look whether it has been initialized, 0.3 us: it has, where there
+# are tensors on a GPU)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
 def _stream(dev: torch.device):
     """The handle of dev's current stream, without the stream object where torch
     can (0.1 instead of 1.9 us of every call)."""
@@ -331,7 +336,7 @@ def _elsewhere(q: torch.Tensor, *ts: Optional[torch.Tensor]) -> bool:
             _need_gpu(q, *ts)
     if i < 0:
         _need_gpu(q)
-    return i != torch.cuda.current_device()
+    return i != _current_device()
 
 
 def _ints(t: Optional[torch.Tensor], name: str, n: int) -> None:
@@ -771,26 +776,27 @@ def mx4_scale_stride(K: int) -> int:
     return (K + 511) // 512 * 16
 
 
+# (called for every layer of every token, as the serving calls)
+def _bytes(t: torch.Tensor, name: str, rows: int, cols: int) -> None:
+    """Checks a contiguous uint8 [rows, cols] tensor."""
+    if t.shape != (rows, cols) or t.dtype is not torch.uint8 or not t.is_contiguous():
+        _check(t, name, (rows, cols), torch.uint8)
+
+
 def _mx4_rows(codes: torch.Tensor, scales: torch.Tensor, name: str) -> Tuple[int, int]:
-    """(rows, K) of an MXFP4 operand."""
-    if codes.dim() != 2 or codes.dtype is not torch.uint8 or not codes.is_contiguous():
-        raise ValueError(f"{name}_codes must be a contiguous uint8 [rows, K/2] tensor, got {codes.dtype} {tuple(codes.shape)}")
-    rows, K = codes.shape[0], 2 * codes.shape[1]
-    want = (rows, mx4_scale_stride(K))
-    if scales.shape != want or scales.dtype is not torch.uint8 or not scales.is_contiguous():
-        raise ValueError(f"{name}_scales must be a contiguous uint8 tensor of shape {want}, got {scales.dtype} {tuple(scales.shape)}")
-    return rows, K
+    """(rows, K/2) of an MXFP4 operand."""
+    shape = codes.shape
+    if len(shape) != 2 or codes.dtype is not torch.uint8 or not codes.is_contiguous():
+        raise ValueError(f"{name}_codes must be a contiguous uint8 [rows, K/2] tensor, got {codes.dtype} {tuple(shape)}")
+    rows, half = shape
+    if scales.shape != (rows, (half + 255) // 256 * 16) or scales.dtype is not torch.uint8 or not scales.is_contiguous():
+        raise ValueError(f"{name}_scales must be a contiguous uint8 tensor of shape {(rows, mx4_scale_stride(2 * half))}, "
+                         f"got {scales.dtype} {tuple(scales.shape)}")
+    return rows, half
 
 
-def _mx4_out(codes, scales, rows: int, K: int, dev):
-    """The given buffers of an MXFP4 result, checked, or new ones."""
-    _check(codes, "codes", (rows, K // 2), torch.uint8)
-    _check(scales, "scales", (rows, mx4_scale_stride(K)), torch.uint8)
-    if codes is None:
-        codes = torch.empty((rows, K // 2), dtype=torch.uint8, device=dev)
-    if scales is None:
-        scales = torch.empty((rows, mx4_scale_stride(K)), dtype=torch.uint8, device=dev)
-    return codes, scales
+def _new_bytes(rows: int, cols: int, dev) -> torch.Tensor:
+    return torch.empty((rows, cols), dtype=torch.uint8, device=dev)
 
 
 def quant_mx4(x: torch.Tensor, codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
@@ -802,16 +808,22 @@ def quant_mx4(x: torch.Tensor, codes: Optional[torch.Tensor] = None, scales: Opt
     if x.dim() != 2:
         raise ValueError("x must be 2-D")
     M, K = x.shape
-    ldx = _rows_of(x, "x", M, K, x.dtype if x.dtype in _CODES else torch.float16)
-    ldv = 0 if values is None else _rows_of(values, "values", M, K, x.dtype)
-    _check(codes, "codes", (M, K // 2), torch.uint8)
-    _check(scales, "scales", (M, mx4_scale_stride(K)), torch.uint8)
+    dt = x.dtype
+    ldx = _rows_of(x, "x", M, K, dt if dt in _CODES else torch.float16)
+    ldv = 0 if values is None else _rows_of(values, "values", M, K, dt)
+    if codes is not None:
+        _bytes(codes, "codes", M, K // 2)
+    if scales is not None:
+        _bytes(scales, "scales", M, mx4_scale_stride(K))
     dev = x.device
     if _elsewhere(x, codes, scales, values):
         with torch.cuda.device(dev):
             return quant_mx4(x, codes, scales, values)
-    codes, scales = _mx4_out(codes, scales, M, K, dev)
-    check(lib().p4q_quant_mx4(_CODES[x.dtype], M, K, x.data_ptr(), ldx, codes.data_ptr(), scales.data_ptr(),
+    if codes is None:
+        codes = _new_bytes(M, K // 2, dev)
+    if scales is None:
+        scales = _new_bytes(M, mx4_scale_stride(K), dev)
+    check(lib().p4q_quant_mx4(_CODES[dt], M, K, x.data_ptr(), ldx, codes.data_ptr(), scales.data_ptr(),
                               _ptr(values), ldv, _stream(dev)))
     return codes, scales
 
@@ -832,7 +844,8 @@ def residual_rmsnorm_quant(x: torch.Tensor, gamma: torch.Tensor, r: Optional[tor
     [M, d], if given, receives what the codes stand for, rounded to x's dtype."""
     if x.dim() != 2:
         raise ValueError("x must be 2-D")
-    if fmt not in ("mx4", "int4"):
+    mx4 = fmt == "mx4"
+    if not mx4 and fmt != "int4":
         raise ValueError(f"fmt must be 'mx4' or 'int4', got {fmt!r}")
     M, d = x.shape
     dt = x.dtype if x.dtype in _CODES else torch.float16
@@ -840,16 +853,21 @@ def residual_rmsnorm_quant(x: torch.Tensor, gamma: torch.Tensor, r: Optional[tor
     for t, name in ((gamma, "gamma"), (post_gamma, "post_gamma"), (gate, "gate")):
         if t is not None and (t.shape != (d,) or t.dtype != dt or not t.is_contiguous()):
             raise ValueError(f"{name} must be a contiguous [d] tensor of x's dtype")
-    if r is None and (h_out is not None or gate is not None or post_gamma is not None or alpha != 1.0):
+    ldr = ldh = ldv = 0
+    if r is not None:
+        ldr = _rows_of(r, "r", M, d, dt)
+        ldh = d if h_out is None else _rows_of(h_out, "h_out", M, d, dt)
+    elif h_out is not None or gate is not None or post_gamma is not None or alpha != 1.0:
         raise ValueError("h_out, gate, post_gamma and alpha need r")
-    ldr = 0 if r is None else _rows_of(r, "r", M, d, dt)
-    ldh = d if h_out is None else _rows_of(h_out, "h_out", M, d, dt)
-    ldv = 0 if values is None else _rows_of(values, "values", M, d, dt)
-    _check(codes, "codes", (M, d // 2), torch.uint8)
-    if fmt == "mx4":
-        _check(scales, "scales", (M, mx4_scale_stride(d)), torch.uint8)
-    else:
-        _check(scales, "scales", (M,), torch.float32)
+    if values is not None:
+        ldv = _rows_of(values, "values", M, d, dt)
+    if codes is not None:
+        _bytes(codes, "codes", M, d // 2)
+    if scales is not None:
+        if mx4:
+            _bytes(scales, "scales", M, mx4_scale_stride(d))
+        else:
+            _check(scales, "scales", (M,), torch.float32)
     dev = x.device
     if _elsewhere(x, gamma, r, post_gamma, gate, h_out, codes, scales, values):
         with torch.cuda.device(dev):
@@ -857,41 +875,46 @@ def residual_rmsnorm_quant(x: torch.Tensor, gamma: torch.Tensor, r: Optional[tor
                                           values)
     if r is not None and h_out is None:
         h_out = torch.empty((M, d), dtype=dt, device=dev)
-    if fmt == "mx4":
-        codes, scales = _mx4_out(codes, scales, M, d, dev)
-    else:
-        if codes is None:
-            codes = torch.empty((M, d // 2), dtype=torch.uint8, device=dev)
-        if scales is None:
-            scales = torch.empty((M,), dtype=torch.float32, device=dev)
+    if codes is None:
+        codes = _new_bytes(M, d // 2, dev)
+    if scales is None:
+        scales = _new_bytes(M, mx4_scale_stride(d), dev) if mx4 else torch.empty((M,), dtype=torch.float32, device=dev)
     check(lib().p4q_residual_rmsnorm_quant(
-        _CODES[dt], P4Q_NORM_MX4 if fmt == "mx4" else P4Q_NORM_INT4, M, d, x.data_ptr(), ldx, _ptr(r), ldr,
-        _ptr(post_gamma), _ptr(gate), alpha, gamma.data_ptr(), eps, clip, _ptr(h_out), ldh, codes.data_ptr(),
-        scales.data_ptr(), _ptr(values), ldv, _stream(dev)))
+        _CODES[dt], P4Q_NORM_MX4 if mx4 else P4Q_NORM_INT4, M, d, x.data_ptr(), ldx, _ptr(r), ldr, _ptr(post_gamma),
+        _ptr(gate), alpha, gamma.data_ptr(), eps, clip, _ptr(h_out), ldh, codes.data_ptr(), scales.data_ptr(),
+        _ptr(values), ldv, _stream(dev)))
     return codes, scales, x if r is None else h_out
 
 
-def _mx4_product(fn: str, pair: int, a_codes, a_scales, w_codes, w_scales, out_dtype, y):
-    M, K = _mx4_rows(a_codes, a_scales, "a")
-    rows, K2 = _mx4_rows(w_codes, w_scales, "w")
-    if K != K2:
+def _mx4_operands(a_codes, a_scales, w_codes, w_scales, pair: int) -> Tuple[int, int, int]:
+    """(M, N, K) of a product, whose weight holds `pair` rows for each output."""
+    M, half = _mx4_rows(a_codes, a_scales, "a")
+    rows, half2 = _mx4_rows(w_codes, w_scales, "w")
+    if half != half2:
         raise ValueError("a_codes and w_codes disagree on K")
-    if rows % pair:
+    if pair == 2 and rows % 2:
         raise ValueError(f"w_codes must hold gate rows and as many up rows, got {rows}")
-    N = rows // pair
-    if y is None:
-        if out_dtype not in _CODES:
-            raise ValueError(f"out_dtype must be fp16 or bf16, got {out_dtype}")
-    else:
-        _check_rows(y, "y", M, N, _F16)
+    return M, rows // pair, 2 * half
+
+
+def _mx4_product(fn, a_codes, a_scales, w_codes, w_scales, pair, out_dtype, y):
+    M, N, K = _mx4_operands(a_codes, a_scales, w_codes, w_scales, pair)
+    if y is not None:
+        shape = y.shape
+        ldy, unit = y.stride() if len(shape) == 2 else (0, 0)
+        if shape != (M, N) or unit != 1 or (M > 1 and ldy < N) or y.dtype not in _CODES:
+            _check_rows(y, "y", M, N, _F16)
+        ldy = max(ldy, N)
+    elif out_dtype not in _CODES:
+        raise ValueError(f"out_dtype must be fp16 or bf16, got {out_dtype}")
     dev = a_codes.device
     if _elsewhere(a_codes, a_scales, w_codes, w_scales, y):
         with torch.cuda.device(dev):
-            return _mx4_product(fn, pair, a_codes, a_scales, w_codes, w_scales, out_dtype, y)
+            return _mx4_product(fn, a_codes, a_scales, w_codes, w_scales, pair, out_dtype, y)
     if y is None:
-        y = torch.empty((M, N), dtype=out_dtype, device=dev)
+        y, ldy = torch.empty((M, N), dtype=out_dtype, device=dev), N
     check(getattr(lib(), fn)(M, N, K, a_codes.data_ptr(), a_scales.data_ptr(), w_codes.data_ptr(), w_scales.data_ptr(),
-                             _CODES[y.dtype], y.data_ptr(), y.stride(0) if M > 1 else max(N, y.stride(0)), _stream(dev)))
+                             _CODES[y.dtype], y.data_ptr(), ldy, _stream(dev)))
     return y
 
 
@@ -900,7 +923,7 @@ def mx4_linear(a_codes: torch.Tensor, a_scales: torch.Tensor, w_codes: torch.Ten
     """MXFP4 linear (p4q_mx4_linear): a (codes [M, K/2], scales) and w (codes
     [N, K/2], scales) as quant_mx4() gives them -> y [M, N] of out_dtype (of y's, if
     given; its rows may be columns of a wider buffer)."""
-    return _mx4_product("p4q_mx4_linear", 1, a_codes, a_scales, w_codes, w_scales, out_dtype, y)
+    return _mx4_product("p4q_mx4_linear", a_codes, a_scales, w_codes, w_scales, 1, out_dtype, y)
 
 
 def mx4_gated_linear(a_codes: torch.Tensor, a_scales: torch.Tensor, w_codes: torch.Tensor, w_scales: torch.Tensor,
@@ -908,7 +931,7 @@ def mx4_gated_linear(a_codes: torch.Tensor, a_scales: torch.Tensor, w_codes: tor
     """Gate and up projection of a feed-forward block in one product
     (p4q_mx4_gated_linear): w holds the gate's N rows, then the up projection's N;
     y [M, N] = SiLU(a w_gate^T) * (a w_up^T)."""
-    return _mx4_product("p4q_mx4_gated_linear", 2, a_codes, a_scales, w_codes, w_scales, out_dtype, y)
+    return _mx4_product("p4q_mx4_gated_linear", a_codes, a_scales, w_codes, w_scales, 2, out_dtype, y)
 
 
 def mx4_gated_linear_quant(a_codes: torch.Tensor, a_scales: torch.Tensor, w_codes: torch.Tensor,
@@ -917,20 +940,19 @@ def mx4_gated_linear_quant(a_codes: torch.Tensor, a_scales: torch.Tensor, w_code
     """mx4_gated_linear() whose result leaves as MXFP4 (p4q_mx4_gated_linear_quant),
     ready for mx4_linear(): (codes uint8 [M, N/2], scales uint8
     [M, mx4_scale_stride(N)]), N a multiple of 32."""
-    M, K = _mx4_rows(a_codes, a_scales, "a")
-    rows, K2 = _mx4_rows(w_codes, w_scales, "w")
-    if K != K2:
-        raise ValueError("a_codes and w_codes disagree on K")
-    if rows % 2:
-        raise ValueError(f"w_codes must hold gate rows and as many up rows, got {rows}")
-    N = rows // 2
-    _check(codes, "codes", (M, N // 2), torch.uint8)
-    _check(scales, "scales", (M, mx4_scale_stride(N)), torch.uint8)
+    M, N, K = _mx4_operands(a_codes, a_scales, w_codes, w_scales, 2)
+    if codes is not None:
+        _bytes(codes, "codes", M, N // 2)
+    if scales is not None:
+        _bytes(scales, "scales", M, mx4_scale_stride(N))
     dev = a_codes.device
     if _elsewhere(a_codes, a_scales, w_codes, w_scales, codes, scales):
         with torch.cuda.device(dev):
             return mx4_gated_linear_quant(a_codes, a_scales, w_codes, w_scales, codes, scales)
-    codes, scales = _mx4_out(codes, scales, M, N, dev)
+    if codes is None:
+        codes = _new_bytes(M, N // 2, dev)
+    if scales is None:
+        scales = _new_bytes(M, mx4_scale_stride(N), dev)
     check(lib().p4q_mx4_gated_linear_quant(M, N, K, a_codes.data_ptr(), a_scales.data_ptr(), w_codes.data_ptr(),
                                            w_scales.data_ptr(), codes.data_ptr(), scales.data_ptr(), _stream(dev)))
     return codes, scales

@@ -20,6 +20,7 @@ namespace p4q {
 namespace {
 
 typedef int v8i __attribute__((ext_vector_type(8)));
+typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 
 // what becomes of the sums
@@ -31,6 +32,13 @@ template <int I>
 __device__ __forceinline__ void mfma_mx4(v4i w, uint32_t sw, v4i a, uint32_t sa, v16f &acc) {
     const v8i W = {w[0], w[1], w[2], w[3], 0, 0, 0, 0}, A = {a[0], a[1], a[2], a[3], 0, 0, 0, 0};
     acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(W, A, acc, 4, 4, I, (int)sw, I, (int)sa);
+}
+
+// the same over 128 values, 16 x 16
+template <int I>
+__device__ __forceinline__ void mfma_mx4_16(v4i w, uint32_t sw, v4i a, uint32_t sa, v4f &acc) {
+    const v8i W = {w[0], w[1], w[2], w[3], 0, 0, 0, 0}, A = {a[0], a[1], a[2], a[3], 0, 0, 0, 0};
+    acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(W, A, acc, 4, 4, I, (int)sw, I, (int)sa);
 }
 
 // (the hardware's exp2 and reciprocal, one unit in the last place each)
@@ -72,122 +80,10 @@ __device__ __forceinline__ void emit8(const Mx4Product &p, int64_t m, int n0, fl
     }
 }
 
-// The 32 codes each of blocks b .. b + 3 of a row, zero past the row's end
-__device__ __forceinline__ void load_blocks(const uint8_t *row, int b, int blocks, v4i (&c)[4]) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        c[i] = v4i{0, 0, 0, 0};
-        if (b + i < blocks) c[i] = *reinterpret_cast<const v4i *>(row + 16 * (int64_t)(b + i));
-    }
-}
-
-// their scale bytes; 0 past the row's end, whatever the padding holds
-__device__ __forceinline__ uint32_t load_scales(const uint8_t *row, int b, int blocks) {
-    const uint32_t s = *reinterpret_cast<const uint32_t *>(row + b);
-    const int left = blocks - b;
-    return left >= 4 ? s : left <= 0 ? 0u : s & ((1u << (8 * left)) - 1u);
-}
-
-// 32 outputs of MB * 32 rows, the eight wavefronts sharing k in steps of 256;
-// their sums meet in LDS in a fixed order.  Operands come straight from memory.
-constexpr int kSkinnyWaves = 8;
-
-template <int EPI, bool BF16, int MB>
-__global__ __launch_bounds__(64 * kSkinnyWaves) void k_mx4_skinny(const Mx4Product p) {
-    constexpr int F = EPI == kLinear ? 1 : 2;
-    constexpr int kGroup = 64 * 4 + 4;                     // floats of 8 consecutive outputs, all lanes
-    __shared__ float red[kSkinnyWaves][F][MB][4][kGroup];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int r = lane & 31, h = lane >> 5;
-    const int n0 = (int)blockIdx.x * 32;
-    const int64_t m0 = (int64_t)blockIdx.y * 32 * MB;
-    const int blocks = p.K / 32, steps = (blocks + 7) / 8;
-    const int64_t kb = p.K / 2;
-
-    const uint8_t *wrow[F], *wsrow[F], *arow[MB], *asrow[MB];
-#pragma unroll
-    for (int f = 0; f < F; ++f) {
-        const int64_t n = min(n0 + r, p.N - 1) + (int64_t)f * p.N;
-        wrow[f] = p.w + n * kb;
-        wsrow[f] = p.ws + n * p.in_stride;
-    }
-#pragma unroll
-    for (int b = 0; b < MB; ++b) {
-        const int64_t m = min(m0 + 32 * b + r, (int64_t)p.M - 1);
-        arow[b] = p.a + m * kb;
-        asrow[b] = p.as + m * p.in_stride;
-    }
-    v16f acc[F][MB];
-#pragma unroll
-    for (int f = 0; f < F; ++f)
-#pragma unroll
-        for (int b = 0; b < MB; ++b) acc[f][b] = v16f{};
-
-    for (int st = wave; st < steps; st += kSkinnyWaves) {
-        const int c0 = 8 * st + 4 * h;
-        v4i w[F][4], a[MB][4];
-        uint32_t sw[F], sa[MB];
-#pragma unroll
-        for (int f = 0; f < F; ++f) {
-            load_blocks(wrow[f], c0, blocks, w[f]);
-            sw[f] = load_scales(wsrow[f], c0, blocks);
-        }
-#pragma unroll
-        for (int b = 0; b < MB; ++b) {
-            load_blocks(arow[b], c0, blocks, a[b]);
-            sa[b] = load_scales(asrow[b], c0, blocks);
-        }
-#pragma unroll
-        for (int f = 0; f < F; ++f)
-#pragma unroll
-            for (int b = 0; b < MB; ++b) {
-                mfma_mx4<0>(w[f][0], sw[f], a[b][0], sa[b], acc[f][b]);
-                mfma_mx4<1>(w[f][1], sw[f], a[b][1], sa[b], acc[f][b]);
-                mfma_mx4<2>(w[f][2], sw[f], a[b][2], sa[b], acc[f][b]);
-                mfma_mx4<3>(w[f][3], sw[f], a[b][3], sa[b], acc[f][b]);
-            }
-    }
-    // lane l holds row m0 + l % 32, outputs 8 g + 4 (l / 32) + 0..3 in registers 4 g ..
-#pragma unroll
-    for (int f = 0; f < F; ++f)
-#pragma unroll
-        for (int b = 0; b < MB; ++b)
-#pragma unroll
-            for (int g = 0; g < 4; ++g)
-                *reinterpret_cast<float4 *>(&red[wave][f][b][g][4 * lane]) =
-                    make_float4(acc[f][b][4 * g], acc[f][b][4 * g + 1], acc[f][b][4 * g + 2], acc[f][b][4 * g + 3]);
-    __syncthreads();
-    for (int t = threadIdx.x; t < 128 * MB; t += 64 * kSkinnyWaves) {
-        const int b = t >> 7, mr = (t >> 2) & 31, g = t & 3;
-        float v[2][8];
-#pragma unroll
-        for (int f = 0; f < F; ++f) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[f][i] = 0.0f;
-#pragma unroll
-            for (int w = 0; w < kSkinnyWaves; ++w)
-#pragma unroll
-                for (int hh = 0; hh < 2; ++hh) {
-                    const float4 x = *reinterpret_cast<const float4 *>(&red[w][f][b][g][4 * (mr + 32 * hh)]);
-                    v[f][4 * hh + 0] += x.x;
-                    v[f][4 * hh + 1] += x.y;
-                    v[f][4 * hh + 2] += x.z;
-                    v[f][4 * hh + 3] += x.w;
-                }
-        }
-        emit8<EPI, BF16>(p, m0 + 32 * b + mr, n0 + 8 * g, v[0], v[1]);
-    }
-    if constexpr (EPI == kGatedQuant) {
-        // the padding behind a row's last block
-        if (n0 + 32 >= p.N && (int)threadIdx.x < 32 * MB && m0 + threadIdx.x < p.M)
-            for (int64_t i = p.N / 32; i < p.out_stride; ++i) p.scales[(m0 + threadIdx.x) * p.out_stride + i] = 0;
-    }
-}
-
 // ---- tiles through LDS -----------------------------------------------------------
 // A work-group of four wavefronts, 2 x 2, computes 64 FM rows by 64 FN weight
 // rows, each wavefront FM x FN fragments of 32 x 32.  k runs in stages of 256
-// values, four steps each; two stages fit in LDS, filled by DMA, and the ring
+// values, four steps each; two stages (RING) in LDS, filled by DMA, and the ring
 // runs on across the tiles of a persistent work-group.
 //  * A stage's row is 128 bytes, one cache line, loaded by 8 lanes: what the DMA
 //    costs is lines touched per instruction, and rows of half a line cost a third
@@ -200,7 +96,7 @@ __global__ __launch_bounds__(64 * kSkinnyWaves) void k_mx4_skinny(const Mx4Produ
 //    stage's steps 0 to 2, during step 0 those of step 3.  So a slot is read in
 //    three steps and has five for its next stage to arrive, whose DMAs are spread
 //    over the products of steps 1 to 3 (over four steps, with less time to arrive,
-//    2% slower).
+//    2% slower).  A ring of four stages gives a lone work-group more.
 //  * Past the row's end the DMA's offsets lie outside the buffer and give codes
 //    of zero, and the scale bytes there are masked; rows past the last are outside
 //    it too.
@@ -220,18 +116,19 @@ __device__ __forceinline__ void unrolled(F &&f) {
 constexpr int kRowBytes = 128;                   // codes of a row in a stage
 constexpr int kRowScales = 16;                   // scale bytes of a row, two stages'
 
-template <int EPI, bool BF16, int FM, int FN>
-__global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void k_mx4_tile(const Mx4Product p, int tiles_m, int tiles_n) {
+template <int EPI, bool BF16, int FM, int FN, int RING>
+__global__ __launch_bounds__(256, FM * FN > 4 || RING > 2 ? 1 : 2) void k_mx4_tile(const Mx4Product p, int tiles_m, int tiles_n) {
     constexpr int BM = 64 * FM, BW = 64 * FN;              // rows of a, of w
     constexpr int BN = EPI == kLinear ? BW : BW / 2;       // outputs: half of w's rows are the gate's
     constexpr int FO = EPI == kLinear ? FN : FN / 2;       // fragments of outputs per wavefront
     constexpr int OFF_W = BM * kRowBytes, STAGE = OFF_W + BW * kRowBytes;
-    constexpr int OFF_SCALES = 2 * STAGE, OFF_SW = BM * kRowScales, SCALES = OFF_SW + BW * kRowScales;
-    constexpr int OFF_OUT = OFF_SCALES + 2 * SCALES;
+    constexpr int OFF_SCALES = RING * STAGE, OFF_SW = BM * kRowScales, SCALES = OFF_SW + BW * kRowScales;
+    constexpr int S_RING = RING / 2 + 1, OFF_OUT = OFF_SCALES + S_RING * SCALES;
     constexpr int EW = FO >= 2 && FM * FN >= 16 ? 2 : 1;   // fragments stored together
     constexpr int OUT_ROW = 64 * EW, OUT_WAVE = EPI == kGatedQuant ? 0 : 32 * OUT_ROW;
     constexpr int CODE_DMAS = 2 * (FM + FN), DMAS = CODE_DMAS + 1;
     static_assert(EPI == kLinear || FN % 2 == 0, "gate and up fragments");
+    static_assert(RING % 2 == 0, "scales of two stages");
     static_assert(FM <= 4 && FN <= 4, "a wavefront's share of the scales is one load");
     __shared__ __attribute__((aligned(1024))) uint8_t smem[OFF_OUT + 4 * OUT_WAVE];
 
@@ -262,7 +159,7 @@ __global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void k_mx4_tile(const M
     const uint32_t c_row = (uint32_t)lane >> 3;
     const uint32_t c_chunk[2] = {((uint32_t)lane & 7u) ^ (c_row >> 1), ((uint32_t)lane & 7u) ^ (c_row >> 1) ^ 4u};
     constexpr uint32_t kOutside = 0x80000000u;
-    int iss_tile = -1, iss_kt = KT2 - 1, iss_slot = 1, sc_tile = -1, sc_kt = KT2 - 2, sc_slot = 1;
+    int iss_tile = -1, iss_kt = KT2 - 1, iss_slot = RING - 1, sc_tile = -1, sc_kt = KT2 - 2, sc_slot = S_RING - 1;
     v4i dA = {}, dW = {}, dSA = {}, dSW = {};
     uint32_t iss_v[2] = {}, iss_lds = 0;
     auto rows_of = [](int64_t total, int64_t first, int most) __attribute__((always_inline)) {
@@ -271,7 +168,7 @@ __global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void k_mx4_tile(const M
     // the place of the next two stages' scales of a
     auto scales_a = [&]() __attribute__((always_inline)) {
         sc_kt += 2;
-        sc_slot ^= 1;
+        if (++sc_slot == S_RING) sc_slot = 0;
         if (sc_kt == KT2) {
             sc_kt = 0;
             ++sc_tile;
@@ -297,7 +194,7 @@ __global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void k_mx4_tile(const M
             dSW = buffer_desc(p.ws + w0 * sb, rw * sb);
         }
         if (iss_kt & 1) scales_a();
-        iss_slot ^= 1;
+        iss_slot = (iss_slot + 1) % RING;
         iss_lds = lds + (uint32_t)iss_slot * STAGE;
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
@@ -368,18 +265,18 @@ __global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void k_mx4_tile(const M
     typedef std::integral_constant<int, 2> c2;
     typedef std::integral_constant<int, 3> c3;
 
-    // the first stage's scales of a, then what two stages before the first would have issued
+    // the first stage's scales of a, then what the stages before the first would have issued
     constexpr int X = FM * FN, PARTS = 3 * X, EARLY = X * DMAS / PARTS;
     scales_a();
     if (lane < 16 * FM) {
         const uint32_t row = (uint32_t)wave * 16 * FM;
         dma16(dSA, (row + (uint32_t)lane) * sb, lds + OFF_SCALES + (uint32_t)sc_slot * SCALES + row * kRowScales);
     }
-    issue_begin();
-    unrolled<DMAS>(issue);
-    issue_begin();
-    unrolled<DMAS>(issue);
-    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(DMAS) : "memory");
+    unrolled<RING>([&](auto) __attribute__((always_inline)) {
+        issue_begin();
+        unrolled<DMAS>(issue);
+    });
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((RING - 1) * DMAS) : "memory");
     uint32_t slot = 0, s_slot = 0;                         // of the stage that is read next
     unrolled<F>([&](auto k) __attribute__((always_inline)) { read_scale(0, 0, k); });
     unrolled<F>([&](auto k) __attribute__((always_inline)) { read_one(0, c0{}, k); });
@@ -406,10 +303,11 @@ __global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void k_mx4_tile(const M
                     issue_begin();
                 }
                 if constexpr (i == 2) {
-                    // the next stage has landed (in order: only what step 1 issued may be outstanding)
-                    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(EARLY) : "memory");
-                    slot ^= 1;
-                    if (kt & 1) s_slot ^= 1;
+                    // the next stage has landed (in order: the ring's others and what step 1 issued
+                    // may be outstanding)
+                    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((RING - 2) * DMAS + EARLY) : "memory");
+                    slot = (slot + 1) % RING;
+                    if ((kt & 1) && ++s_slot == S_RING) s_slot = 0;
                 }
                 __builtin_amdgcn_sched_barrier(0);
                 unrolled<FM * FN>([&](auto x_c) __attribute__((always_inline)) {
@@ -523,25 +421,242 @@ __global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void k_mx4_tile(const M
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // no DMA into LDS past the end
 }
 
-template <int EPI, bool BF16, int FM, int FN>
+// ---- few rows: weights streamed past them ------------------------------------------
+// A work-group computes 16 FO outputs of 16 MB rows.  Its wavefronts share k in
+// contiguous runs of stages of 256 values and need nothing of each other until
+// their sums meet in LDS, in a fixed order: each has a ring of two stages of its
+// own, filled by DMA, and waits for it alone.
+//  * A fragment is 16 rows; a stage's 128 bytes of a row lie as in the tiles above.
+//    In a product of 128 values lane l takes the blocks 2 (l / 16) and, in the
+//    second, 2 (l / 16) + 1 of row l % 16.
+//  * Scale bytes come 32 per row, for four stages at once, into two buffers.
+constexpr int kRowsRing = 2, kRowsGroup = 4;
+
+template <int EPI, bool BF16, int MB, int NW>
+__global__ __launch_bounds__(64 * NW) void k_mx4_rows(const Mx4Product p) {
+    constexpr int FO = EPI == kGatedQuant ? 2 : 1;         // fragments of outputs (32: a block to quantize)
+    constexpr int F = EPI == kLinear ? FO : 2 * FO;        // of w: the gate's, then the up rows'
+    constexpr int FRAG = 16 * kRowBytes, STAGE = (F + MB) * FRAG;
+    constexpr int SC_ROW = 8 * kRowsGroup, SC_FRAG = 16 * SC_ROW, GROUP = (F + MB) * SC_FRAG;
+    constexpr int OFF_SC = kRowsRing * STAGE, PER_WAVE = OFF_SC + 2 * GROUP;
+    constexpr int DMAS = 2 * (F + MB);
+    constexpr int RED = NW * F * MB * 1024;
+    constexpr int BYTES = NW * PER_WAVE > RED ? NW * PER_WAVE : RED;
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[BYTES];
+    const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int n0 = (int)blockIdx.x * 16 * FO;
+    const int64_t m0 = (int64_t)blockIdx.y * 16 * MB;
+    const int blocks = p.K / 32, KT = (blocks + 7) / 8;
+    // (an even number of stages each, so that their scale bytes start 16 bytes apart)
+    const int per = ((KT + NW - 1) / NW + 1) & ~1, first = wave * per, end = min(KT, first + per);
+    const uint32_t kb = (uint32_t)p.K / 2, sb = (uint32_t)p.in_stride;
+
+    // one buffer for each operand; a fragment's rows past the last lie outside it
+    const uint32_t rm = (uint32_t)min((int64_t)p.M - m0, (int64_t)16 * MB), rn = (uint32_t)min(p.N - n0, 16 * FO);
+    const v4i dA = buffer_desc(p.a + m0 * kb, rm * kb), dSA = buffer_desc(p.as + m0 * sb, rm * sb);
+    v4i dW[2], dSW[2];
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+        const int64_t row = n0 + (EPI == kLinear ? 0 : (int64_t)g * p.N);
+        dW[g] = buffer_desc(p.w + row * kb, rn * kb);
+        dSW[g] = buffer_desc(p.ws + row * sb, rn * sb);
+    }
+    const uint32_t lds = lds_addr(smem) + (uint32_t)wave * PER_WAVE;
+    const uint32_t c_row = (uint32_t)lane >> 3;
+    const uint32_t c_chunk[2] = {((uint32_t)lane & 7u) ^ (c_row >> 1), ((uint32_t)lane & 7u) ^ (c_row >> 1) ^ 4u};
+    constexpr uint32_t kOutside = 0x80000000u;
+    auto issue = [&](int st, int slot) __attribute__((always_inline)) {
+        const uint32_t to = lds + (uint32_t)slot * STAGE;
+        uint32_t v[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const uint32_t c = (uint32_t)st * 8u + c_chunk[x];
+            v[x] = st < end && c < (uint32_t)blocks ? (c_row + 8 * x) * kb + c * 16u : kOutside;
+        }
+#pragma unroll
+        for (int f = 0; f < F; ++f)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) dma16(dW[f / FO], v[x] + (uint32_t)(f % FO) * 16u * kb, to + f * FRAG + x * 1024);
+#pragma unroll
+        for (int b = 0; b < MB; ++b)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) dma16(dA, v[x] + (uint32_t)b * 16u * kb, to + (F + b) * FRAG + x * 1024);
+    };
+    // the scale bytes of stages st .. st + 3 (of the last, as far as a row of them goes)
+    auto issue_scales = [&](int st, int buf) __attribute__((always_inline)) {
+        const uint32_t to = lds + OFF_SC + (uint32_t)buf * GROUP;
+        const uint32_t at = (uint32_t)st * 8u + ((uint32_t)lane & 1u) * 16u;
+        const uint32_t v = st < end && at < sb ? ((uint32_t)lane >> 1) * sb + at : kOutside;
+        if (lane < 32) {
+#pragma unroll
+            for (int f = 0; f < F; ++f) dma16(dSW[f / FO], v + (uint32_t)(f % FO) * 16u * sb, to + f * SC_FRAG);
+#pragma unroll
+            for (int b = 0; b < MB; ++b) dma16(dSA, v + (uint32_t)b * 16u * sb, to + (F + b) * SC_FRAG);
+        }
+    };
+
+    v4f acc[F][MB];
+#pragma unroll
+    for (int f = 0; f < F; ++f)
+#pragma unroll
+        for (int b = 0; b < MB; ++b) acc[f][b] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    issue_scales(first, 0);
+    issue(first, 0);
+    issue(first + 1, 1);
+    const uint8_t *mine = smem + wave * PER_WAVE;
+    const uint32_t at0 = (uint32_t)(r * kRowBytes + (((2 * q) ^ (r >> 1)) << 4));
+    const uint32_t at1 = (uint32_t)(r * kRowBytes + (((2 * q + 1) ^ (r >> 1)) << 4));
+    for (int st = first; st < end; ++st) {
+        const int i = st - first, slot = i % kRowsRing, group = i / kRowsGroup, in_group = i % kRowsGroup;
+        // in order: with the next stage's loads outstanding this one's have landed,
+        // and its scale bytes before them
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(DMAS) : "memory");
+        v4i x0[F + MB], x1[F + MB];
+        uint32_t s[F + MB];
+        const int left = blocks - 8 * st - 2 * q;
+        const uint32_t mask = left >= 2 ? 0xFFFFu : left == 1 ? 0xFFu : 0u;
+#pragma unroll
+        for (int f = 0; f < F + MB; ++f) {
+            x0[f] = *reinterpret_cast<const v4i *>(mine + slot * STAGE + f * FRAG + at0);
+            x1[f] = *reinterpret_cast<const v4i *>(mine + slot * STAGE + f * FRAG + at1);
+            s[f] = mask & *reinterpret_cast<const uint16_t *>(mine + OFF_SC + (group & 1) * GROUP + f * SC_FRAG +
+                                                              r * SC_ROW + in_group * 8 + 2 * q);
+        }
+        // held before the slot takes the stage after the next
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        issue(st + kRowsRing, slot);
+        if (in_group == 0) issue_scales(st + kRowsGroup, (group + 1) & 1);
+#pragma unroll
+        for (int f = 0; f < F; ++f)
+#pragma unroll
+            for (int b = 0; b < MB; ++b) {
+                mfma_mx4_16<0>(x0[f], s[f], x0[F + b], s[F + b], acc[f][b]);
+                mfma_mx4_16<1>(x1[f], s[f], x1[F + b], s[F + b], acc[f][b]);
+            }
+    }
+    // lane l holds row m0 + l % 16, outputs 4 (l / 16) + 0..3 of a fragment
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // no DMA into LDS from here on
+    __syncthreads();
+    float4 *red = reinterpret_cast<float4 *>(smem);
+#pragma unroll
+    for (int f = 0; f < F; ++f)
+#pragma unroll
+        for (int b = 0; b < MB; ++b)
+            red[((wave * F + f) * MB + b) * 64 + lane] = make_float4(acc[f][b][0], acc[f][b][1], acc[f][b][2], acc[f][b][3]);
+    __syncthreads();
+    constexpr int PER_ROW = 2 * FO;                        // threads of a row, 8 outputs each
+    const int t = (int)threadIdx.x;
+    if (t < 16 * MB * PER_ROW) {
+        const int g = t % PER_ROW, row = t / PER_ROW, b = row >> 4;
+        float v[2][8];
+#pragma unroll
+        for (int f = 0; f < 2; ++f) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[f][e] = 0.0f;
+            if (f * FO >= F) continue;
+            const int frag = f * FO + (g >> 1);
+#pragma unroll
+            for (int w = 0; w < NW; ++w)
+#pragma unroll
+                for (int hh = 0; hh < 2; ++hh) {
+                    const float4 x = red[((w * F + frag) * MB + b) * 64 + (2 * (g & 1) + hh) * 16 + (row & 15)];
+                    v[f][4 * hh + 0] += x.x;
+                    v[f][4 * hh + 1] += x.y;
+                    v[f][4 * hh + 2] += x.z;
+                    v[f][4 * hh + 3] += x.w;
+                }
+        }
+        emit8<EPI, BF16>(p, m0 + row, n0 + 8 * g, v[0], v[1]);
+    }
+    if constexpr (EPI == kGatedQuant) {
+        // the padding behind a row's last block
+        if (n0 + 32 >= p.N && t < 16 * MB && m0 + t < p.M)
+            for (int64_t i = p.N / 32; i < p.out_stride; ++i) p.scales[(m0 + t) * p.out_stride + i] = 0;
+    }
+}
+
+// ---- which kernel ------------------------------------------------------------------
+// Estimated microseconds of each, from measurements on 256 CUs (below: what they
+// were fitted to), and the least of them taken.  What decides is how the tiles fall
+// into rounds: a tile of 256 x 256 needs half the L2 traffic of four of 128 x 128
+// and idles the CUs that the last round leaves out.
+struct TileCost {
+    double idle, busy;                           // us a stage, of the first tile on the device and with every CU at work
+    double epilogue;                             // us a round
+    int per_cu;                                  // work-groups
+};
+inline double tile_cost(const Mx4Product &p, int bm, int bn, const TileCost &c, int cus) {
+    const int64_t tiles = (((int64_t)p.M + bm - 1) / bm) * (((int64_t)p.N + bn - 1) / bn);
+    const int64_t slots = (int64_t)cus * c.per_cu, whole = tiles / slots;
+    const int stages = (p.K / 32 + 7) / 8;
+    double us = 2.5 + (double)whole * (c.epilogue + stages * c.busy);
+    if (const int64_t left = tiles % slots) {
+        // two on a CU take nearly twice as long as one, whether or not every CU has two
+        const bool paired = left > cus;
+        us += c.epilogue + stages * (paired ? c.busy - 0.2 * (double)(slots - left) / cus
+                                            : c.idle + (c.busy / c.per_cu - c.idle) * (double)left / cus);
+    }
+    return us;
+}
+// the rows kernel: what its work-groups load, 15 MB a microsecond
+inline double rows_cost(const Mx4Product &p, int mb, int frags, int outputs) {
+    const double groups = ((p.N + outputs - 1) / outputs) * (double)((p.M + 16 * mb - 1) / (16 * mb));
+    return 3.5 + groups * ((p.K / 32 + 7) / 8) * (frags + mb) * 2176.0 / 15e6;
+}
+
+// all outputs by tiles of 64 FM x 64 FN (gated: 32 FN)
+template <int EPI, bool BF16, int FM, int FN, int RING>
 hipError_t launch_tile(const Mx4Product &p, hipStream_t stream) {
     constexpr int BM = 64 * FM, BN = (EPI == kLinear ? 64 : 32) * FN;
     const int tiles_m = (int)(((int64_t)p.M + BM - 1) / BM), tiles_n = (p.N + BN - 1) / BN;
     const int64_t T = (int64_t)tiles_m * tiles_n;
-    const int64_t grid = std::min<int64_t>(T, (int64_t)device_cus() * (FM * FN >= 16 ? 1 : 2));
-    hipLaunchKernelGGL((k_mx4_tile<EPI, BF16, FM, FN>), dim3((unsigned)grid), dim3(256), 0, stream, p, tiles_m, tiles_n);
+    const int64_t grid = std::min<int64_t>(T, (int64_t)device_cus() * (FM * FN > 4 || RING > 2 ? 1 : 2));
+    hipLaunchKernelGGL((k_mx4_tile<EPI, BF16, FM, FN, RING>), dim3((unsigned)grid), dim3(256), 0, stream, p, tiles_m, tiles_n);
+    return hipGetLastError();
+}
+
+// Two wavefronts a work-group where there are two for each CU or more, else four:
+// 32 rows at N = 12288, K = 4096 (768 work-groups) 6.7 against 9.4 us, one row at
+// N = 5120, K = 13824 (320) 11.1 against 8.2.
+template <int EPI, bool BF16, int MB>
+hipError_t launch_rows(const Mx4Product &p, int cus, hipStream_t stream) {
+    constexpr int NO = EPI == kGatedQuant ? 32 : 16;
+    const dim3 grid((unsigned)((p.N + NO - 1) / NO), (unsigned)((p.M + 16 * MB - 1) / (16 * MB)));
+    if ((int64_t)grid.x * grid.y >= 2 * cus)
+        hipLaunchKernelGGL((k_mx4_rows<EPI, BF16, MB, 2>), grid, dim3(128), 0, stream, p);
+    else
+        hipLaunchKernelGGL((k_mx4_rows<EPI, BF16, MB, 4>), grid, dim3(256), 0, stream, p);
     return hipGetLastError();
 }
 
 template <int EPI, bool BF16>
 hipError_t launch_typed(const Mx4Product &p, hipStream_t stream) {
-    if (p.M > 64) {
-        const int64_t tiles = (((int64_t)p.M + 255) / 256) * ((p.N + (EPI == kLinear ? 255 : 127)) / (EPI == kLinear ? 256 : 128));
-        return tiles >= device_cus() ? launch_tile<EPI, BF16, 4, 4>(p, stream) : launch_tile<EPI, BF16, 2, 2>(p, stream);
+    constexpr int W = EPI == kLinear ? 64 : 32;            // outputs of 64 weight rows
+    constexpr int NO = EPI == kGatedQuant ? 32 : 16, F = EPI == kLinear ? 1 : EPI == kGated ? 2 : 4;
+    const int cus = device_cus();
+    if (p.M <= 16) return launch_rows<EPI, BF16, 1>(p, cus, stream);
+    double least = p.M <= 1024 ? rows_cost(p, 2, F, NO) : 1e30;
+    int best = 0;
+    auto offer = [&](int which, int bm, int bn, const TileCost &c) {
+        const double us = tile_cost(p, bm, bn, c, cus);
+        if (us < least) least = us, best = which;
+    };
+    if (EPI == kLinear) offer(11, 64, 64, {0.38, 0.42, 1.0, 1});
+    if (EPI == kLinear) offer(12, 64, 128, {0.5, 0.95, 1.0, 2});
+    else offer(12, 64, 64, {0.5, 0.55, 1.0, 1});
+    offer(22, 128, 2 * W, {0.55, 1.2, 1.5, 2});
+    offer(34, 192, 4 * W, {1.02, 1.42, 3.0, 1});
+    offer(44, 256, 4 * W, {1.18, 1.73, 4.0, 1});
+    switch (best) {
+        case 0: return launch_rows<EPI, BF16, 2>(p, cus, stream);
+        case 11:
+            if constexpr (EPI == kLinear) return launch_tile<EPI, BF16, 1, 1, 4>(p, stream);
+        case 12: return launch_tile<EPI, BF16, 1, 2, EPI == kLinear ? 2 : 4>(p, stream);
+        case 22: return launch_tile<EPI, BF16, 2, 2, 2>(p, stream);
+        case 34: return launch_tile<EPI, BF16, 3, 4, 2>(p, stream);
+        default: return launch_tile<EPI, BF16, 4, 4, 2>(p, stream);
     }
-    const dim3 grid((unsigned)((p.N + 31) / 32), (unsigned)(((int64_t)p.M + 31) / 32));
-    hipLaunchKernelGGL((k_mx4_skinny<EPI, BF16, 1>), grid, dim3(64 * kSkinnyWaves), 0, stream, p);
-    return hipGetLastError();
 }
 
 }  // namespace

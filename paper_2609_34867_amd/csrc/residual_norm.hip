@@ -24,16 +24,33 @@
 namespace p4q {
 namespace {
 
-constexpr int kThreads = 256;
+// v of lane ^ M, M < 16 (wave_ops.h)
+template <int M>
+__device__ __forceinline__ double lane_xor_f64(double v) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, v);
+    return __builtin_bit_cast(double, (uint64_t)lane_xor<M>((uint32_t)u) | (uint64_t)lane_xor<M>((uint32_t)(u >> 32)) << 32);
+}
 
+__device__ __forceinline__ double lane_read_f64(double v, int lane) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)u, lane);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(u >> 32), lane);
+    return __builtin_bit_cast(double, (uint64_t)lo | (uint64_t)hi << 32);
+}
+
+// Sum over a work-group of WAVES wavefronts, in a fixed order.
+template <int WAVES>
 __device__ __forceinline__ double block_sum(double s, double *buf) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
+    s += lane_xor_f64<1>(s);
+    s += lane_xor_f64<2>(s);
+    s += lane_xor_f64<4>(s);
+    s += lane_xor_f64<8>(s);
+    s = (lane_read_f64(s, 0) + lane_read_f64(s, 16)) + (lane_read_f64(s, 32) + lane_read_f64(s, 48));
     if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = s;
     __syncthreads();
     double t = 0.0;
 #pragma unroll
-    for (int i = 0; i < kThreads / 64; ++i) t += buf[i];
+    for (int i = 0; i < WAVES; ++i) t += buf[i];
     return t;
 }
 
@@ -53,10 +70,11 @@ __device__ __forceinline__ void unpack8(uint4 w, float (&v)[8]) {
     }
 }
 
-template <int CH, bool BF16, bool INT4, bool CLIP1>
-__global__ __launch_bounds__(kThreads) void k_residual_rmsnorm_quant(const ResidualNorm a) {
-    __shared__ double s_r[kThreads / 64], s_h[kThreads / 64];
-    __shared__ uint32_t s_max[kThreads / 64];
+template <int NT, int CH, bool BF16, bool INT4, bool CLIP1>
+__global__ __launch_bounds__(NT) void k_residual_rmsnorm_quant(const ResidualNorm a) {
+    constexpr int WAVES = NT / 64;
+    __shared__ double s_r[WAVES], s_h[WAVES];
+    __shared__ uint32_t s_max[WAVES];
     const int64_t row = blockIdx.x;
     const int t = threadIdx.x;
     const int chunks = a.d / 8;
@@ -66,7 +84,7 @@ __global__ __launch_bounds__(kThreads) void k_residual_rmsnorm_quant(const Resid
     uint4 h[CH], r[CH], g[CH];
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-        const int q = t + kThreads * c;
+        const int q = t + NT * c;
         const bool in = q < chunks;
         h[c] = in ? load_nt(row_of(a.x, a.ldx) + q) : zero;
         r[c] = in && a.r ? load_nt(row_of(a.r, a.ldr) + q) : zero;
@@ -83,12 +101,12 @@ __global__ __launch_bounds__(kThreads) void k_residual_rmsnorm_quant(const Resid
 #pragma unroll
                 for (int i = 0; i < 8; ++i) ss = __builtin_fma((double)v[i], (double)v[i], ss);
             }
-            ss = block_sum(ss, s_r);
+            ss = block_sum<WAVES>(ss, s_r);
             inv = inverse_rms(ss, a.d, a.eps);
         }
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const int q = t + kThreads * c;
+            const int q = t + NT * c;
             if (q >= chunks) continue;
             float x[8], v[8], p[8], e[8], o[8];
             unpack8<BF16>(h[c], x);
@@ -124,11 +142,14 @@ __global__ __launch_bounds__(kThreads) void k_residual_rmsnorm_quant(const Resid
         const uint32_t mw = wave_max_u32(__float_as_uint(am));
         if ((t & 63) == 0) s_max[t >> 6] = mw;
     }
-    ss = block_sum(ss, s_h);
+    ss = block_sum<WAVES>(ss, s_h);
     const double inv = inverse_rms(ss, a.d, a.eps);
 
     if constexpr (INT4) {
-        const float top = __uint_as_float(max(max(s_max[0], s_max[1]), max(s_max[2], s_max[3])));
+        uint32_t mw = s_max[0];
+#pragma unroll
+        for (int i = 1; i < WAVES; ++i) mw = max(mw, s_max[i]);
+        const float top = __uint_as_float(mw);
         const float s = row_scale<CLIP1>(top, a.clip);
         const float scale = s == 0.0f ? 0.0f : (float)((double)s * inv);
         if (t == 0) static_cast<float *>(a.scales)[row] = scale;
@@ -136,7 +157,7 @@ __global__ __launch_bounds__(kThreads) void k_residual_rmsnorm_quant(const Resid
         const float rs = tiny ? 0.0f : 1.0f / s;
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const int q = t + kThreads * c;
+            const int q = t + NT * c;
             float u[8], w8[8];
             unpack8<BF16>(h[c], u);
             unpack8<BF16>(g[c], w8);
@@ -173,7 +194,7 @@ __global__ __launch_bounds__(kThreads) void k_residual_rmsnorm_quant(const Resid
         uint8_t *scales = static_cast<uint8_t *>(a.scales) + row * a.scale_stride;
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const int q = t + kThreads * c;
+            const int q = t + NT * c;
             float u[8], w8[8];
             unpack8<BF16>(h[c], u);
             unpack8<BF16>(g[c], w8);
@@ -195,26 +216,36 @@ __global__ __launch_bounds__(kThreads) void k_residual_rmsnorm_quant(const Resid
     }
 }
 
-template <int CH, bool BF16>
+template <int NT, int CH, bool BF16>
 hipError_t launch_ch(p4q_norm_format fmt, const ResidualNorm &a, hipStream_t stream) {
     auto go = [&](auto kern) {
-        hipLaunchKernelGGL(kern, dim3(a.M), dim3(kThreads), 0, stream, a);
+        hipLaunchKernelGGL(kern, dim3(a.M), dim3(NT), 0, stream, a);
         return hipGetLastError();
     };
-    if (fmt == P4Q_NORM_MX4) return go(k_residual_rmsnorm_quant<CH, BF16, false, true>);
-    return a.clip == 1.0f ? go(k_residual_rmsnorm_quant<CH, BF16, true, true>)
-                          : go(k_residual_rmsnorm_quant<CH, BF16, true, false>);
+    if (fmt == P4Q_NORM_MX4) return go(k_residual_rmsnorm_quant<NT, CH, BF16, false, true>);
+    return a.clip == 1.0f ? go(k_residual_rmsnorm_quant<NT, CH, BF16, true, true>)
+                          : go(k_residual_rmsnorm_quant<NT, CH, BF16, true, false>);
 }
+
+// 256 threads a row where there are rows enough to fill the device (kFew per CU);
+// else a row's latency counts, and it gets a thread per 16 bytes, or per 32.
+constexpr int kFew = 4;
 
 template <bool BF16>
 hipError_t launch_typed(p4q_norm_format fmt, const ResidualNorm &a, hipStream_t stream) {
-    const int per = (a.d / 8 + kThreads - 1) / kThreads;  // d <= 16384: at most 8
-    if (per <= 1) return launch_ch<1, BF16>(fmt, a, stream);
-    if (per <= 2) return launch_ch<2, BF16>(fmt, a, stream);
-    if (per <= 3) return launch_ch<3, BF16>(fmt, a, stream);
-    if (per <= 4) return launch_ch<4, BF16>(fmt, a, stream);
-    if (per <= 6) return launch_ch<6, BF16>(fmt, a, stream);
-    return launch_ch<8, BF16>(fmt, a, stream);
+    const int chunks = a.d / 8;                            // at most 2048
+    if (chunks > 256 && a.M <= kFew * device_cus()) {
+        if (chunks <= 512) return launch_ch<512, 1, BF16>(fmt, a, stream);
+        if (chunks <= 1024) return launch_ch<1024, 1, BF16>(fmt, a, stream);
+        return launch_ch<1024, 2, BF16>(fmt, a, stream);
+    }
+    const int per = (chunks + 255) / 256;
+    if (per <= 1) return launch_ch<256, 1, BF16>(fmt, a, stream);
+    if (per <= 2) return launch_ch<256, 2, BF16>(fmt, a, stream);
+    if (per <= 3) return launch_ch<256, 3, BF16>(fmt, a, stream);
+    if (per <= 4) return launch_ch<256, 4, BF16>(fmt, a, stream);
+    if (per <= 6) return launch_ch<256, 6, BF16>(fmt, a, stream);
+    return launch_ch<256, 8, BF16>(fmt, a, stream);
 }
 
 }  // namespace
