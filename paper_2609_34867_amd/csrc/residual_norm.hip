@@ -54,10 +54,26 @@ __device__ __forceinline__ double block_sum(double s, double *buf) {
     return t;
 }
 
-// 1 / rms of a row; a row of zeros at eps = 0 stays one of zeros
+// 1 / rms of a row; a row of zeros at eps = 0 stays one of zeros.  The hardware's
+// estimate (at least 22 bits) and one step of third order, within a few units of
+// 2^-53: a twentieth of the instructions of a root and a division.
 __device__ __forceinline__ double inverse_rms(double ss, int d, float eps) {
-    const double ms = ss / (double)d + (double)eps;
-    return ms == 0.0 ? 0.0 : 1.0 / __builtin_sqrt(ms);
+    const double ms = ss * (1.0 / (double)d) + (double)eps;
+    double y = __builtin_amdgcn_rsq(ms);
+    if (y > 0.0) {                                         // neither infinite nor a NaN
+        const double e = __builtin_fma(-ms * y, y, 1.0);
+        y = __builtin_fma(y * e, __builtin_fma(0.375, e, 0.5), y);
+    }
+    return ms == 0.0 ? 0.0 : y;
+}
+
+// 16 bytes, as one access (uint4 goes as four where a condition is about it)
+__device__ __forceinline__ uint4 load16(const uint16_t *p, int q) {
+    const u32x4 v = reinterpret_cast<const u32x4 *>(p)[q];
+    return make_uint4(v.x, v.y, v.z, v.w);
+}
+__device__ __forceinline__ void store16(uint16_t *p, int q, uint4 v) {
+    reinterpret_cast<u32x4 *>(p)[q] = u32x4{v.x, v.y, v.z, v.w};
 }
 
 template <bool BF16>
@@ -81,15 +97,20 @@ __global__ __launch_bounds__(NT) void k_residual_rmsnorm_quant(const ResidualNor
     const uint4 zero = make_uint4(0, 0, 0, 0);
     auto row_of = [&](const uint16_t *p, int64_t ld) { return reinterpret_cast<const uint4 *>(p + row * ld); };
 
-    uint4 h[CH], r[CH], g[CH];
+    uint4 h[CH], r[CH], g[CH], pg[CH], gt[CH];
+    // (lanes past the row's end load its first 16 bytes, and hold zeros for them)
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-        const int q = t + NT * c;
-        const bool in = q < chunks;
-        h[c] = in ? load_nt(row_of(a.x, a.ldx) + q) : zero;
-        r[c] = in && a.r ? load_nt(row_of(a.r, a.ldr) + q) : zero;
-        g[c] = in ? reinterpret_cast<const uint4 *>(a.gamma)[q] : zero;
+        const int q = t + NT * c < chunks ? t + NT * c : 0;
+        h[c] = load_nt(row_of(a.x, a.ldx) + q);
+        g[c] = load16(a.gamma, q);
+        if (a.r) r[c] = load_nt(row_of(a.r, a.ldr) + q);
+        if (a.post) pg[c] = load16(a.post, q);
+        if (a.gate) gt[c] = load16(a.gate, q);
     }
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+        if (t + NT * c >= chunks) h[c] = r[c] = zero;
     if (a.r) {
         double inv = 0.0;
         if (a.post) {
@@ -104,24 +125,42 @@ __global__ __launch_bounds__(NT) void k_residual_rmsnorm_quant(const ResidualNor
             ss = block_sum<WAVES>(ss, s_r);
             inv = inverse_rms(ss, a.d, a.eps);
         }
+        const double f = a.post ? inv * (double)a.alpha : (double)a.alpha;
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int q = t + NT * c;
-            if (q >= chunks) continue;
             float x[8], v[8], p[8], e[8], o[8];
             unpack8<BF16>(h[c], x);
             unpack8<BF16>(r[c], v);
-            if (a.post) unpack8<BF16>(reinterpret_cast<const uint4 *>(a.post)[q], p);
-            if (a.gate) unpack8<BF16>(reinterpret_cast<const uint4 *>(a.gate)[q], e);
+            if (a.post) unpack8<BF16>(pg[c], p);
+            if (a.gate) unpack8<BF16>(gt[c], e);
+            if (!a.post && (!BF16 || !a.gate)) {
+                // r, or the product of two fp16 numbers, is exact in fp32 and the fma
+                // rounds once
+                if (a.gate) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                double z = (double)v[i];
-                if (a.post) z = z * inv * (double)p[i];
-                if (a.gate) z *= (double)e[i];
-                o[i] = (float)((double)x[i] + (double)a.alpha * z);
+                    for (int i = 0; i < 8; ++i) v[i] *= e[i];
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) o[i] = __builtin_fmaf(a.alpha, v[i], x[i]);
+            } else if constexpr (BF16) {
+                // (products of two bfloat16 numbers may leave the range of fp32)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    double w = a.post ? (double)p[i] : 1.0;
+                    if (a.gate) w *= (double)e[i];
+                    o[i] = (float)__builtin_fma((double)v[i] * f, w, (double)x[i]);
+                }
+            } else {
+                if (a.gate) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) p[i] *= e[i];          // exact
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) o[i] = (float)__builtin_fma((double)v[i] * f, (double)p[i], (double)x[i]);
             }
             h[c] = round16x8<BF16>(o);
-            reinterpret_cast<uint4 *>(a.h_out + row * a.ldh)[q] = h[c];
+            if (q < chunks) store16(a.h_out + row * a.ldh, q, h[c]);
         }
     }
 
@@ -186,7 +225,7 @@ __global__ __launch_bounds__(NT) void k_residual_rmsnorm_quant(const ResidualNor
                     float v[8];
 #pragma unroll
                     for (int k = 0; k < 8; ++k) v[k] = (float)((int)(packed << (28 - 4 * k)) >> 28) * scale;
-                    reinterpret_cast<uint4 *>(a.values + row * a.ldv)[q] = round16x8<BF16>(v);
+                    store16(a.values + row * a.ldv, q, round16x8<BF16>(v));
                 }
             }
         }
@@ -199,7 +238,10 @@ __global__ __launch_bounds__(NT) void k_residual_rmsnorm_quant(const ResidualNor
             unpack8<BF16>(h[c], u);
             unpack8<BF16>(g[c], w8);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) u[i] = (float)((double)u[i] * (double)w8[i] * inv);
+            for (int i = 0; i < 8; ++i) {
+                const double z = BF16 ? (double)u[i] * (double)w8[i] : (double)(u[i] * w8[i]);
+                u[i] = (float)(z * inv);
+            }
             uint32_t byte;
             const uint32_t packed = mx4_quantize(u, byte);
             if (q < chunks) {
@@ -207,7 +249,7 @@ __global__ __launch_bounds__(NT) void k_residual_rmsnorm_quant(const ResidualNor
                 reinterpret_cast<uint32_t *>(a.codes)[row * chunks + q] = packed;
                 if (a.values) {
                     mx4_values(packed, byte, u);
-                    reinterpret_cast<uint4 *>(a.values + row * a.ldv)[q] = round16x8<BF16>(u);
+                    store16(a.values + row * a.ldv, q, round16x8<BF16>(u));
                 }
             }
         }
@@ -227,14 +269,14 @@ hipError_t launch_ch(p4q_norm_format fmt, const ResidualNorm &a, hipStream_t str
                           : go(k_residual_rmsnorm_quant<NT, CH, BF16, true, false>);
 }
 
-// 256 threads a row where there are rows enough to fill the device (kFew per CU);
-// else a row's latency counts, and it gets a thread per 16 bytes, or per 32.
-constexpr int kFew = 4;
+// 256 threads a row; where there is at most one row for each CU its latency counts,
+// and it gets a thread per 16 bytes, or per 32 (one row of 4096: 3.3 against 4.0 us;
+// 693 rows of 5120: 14.8 against 13.0).
 
 template <bool BF16>
 hipError_t launch_typed(p4q_norm_format fmt, const ResidualNorm &a, hipStream_t stream) {
     const int chunks = a.d / 8;                            // at most 2048
-    if (chunks > 256 && a.M <= kFew * device_cus()) {
+    if (chunks > 256 && a.M <= device_cus()) {
         if (chunks <= 512) return launch_ch<512, 1, BF16>(fmt, a, stream);
         if (chunks <= 1024) return launch_ch<1024, 1, BF16>(fmt, a, stream);
         return launch_ch<1024, 2, BF16>(fmt, a, stream);
