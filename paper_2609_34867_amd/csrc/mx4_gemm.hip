@@ -577,10 +577,15 @@ __global__ __launch_bounds__(64 * NW) void k_mx4_rows(const Mx4Product p) {
 }
 
 // ---- which kernel ------------------------------------------------------------------
-// Estimated microseconds of each, from measurements on 256 CUs (below: what they
-// were fitted to), and the least of them taken.  What decides is how the tiles fall
-// into rounds: a tile of 256 x 256 needs half the L2 traffic of four of 128 x 128
-// and idles the CUs that the last round leaves out.
+// Each kernel's time is estimated and the least taken.  What decides is how the
+// tiles fall into rounds and what a tile loads: one of 256 x 256 needs half of what
+// four of 128 x 128 load, and the last round may leave most CUs idle.  The numbers
+// are fitted to measurements on 256 CUs at M = 48 .. 11264 and (N, K) from (4096, 4096)
+// to (15360, 5120) and gated (13824, 5120), where the kernel taken was within 3% of
+// the best one at most sizes and 8% behind it at worst.  For example N = 12288,
+// K = 4096: 64 rows 10.2 us by 64 x 64 tiles (16.4 as few rows, 13.1 by 128 x 128);
+// 384 rows 18.1 by 128 x 192 (20.1, 23.9 by 192 x 256); 704 rows 25.2 by 192 x 192
+// (31.6 by 128 x 128); 4096 rows 103.3 by 256 x 256 (123.9).
 struct TileCost {
     double idle, busy;                           // us a stage, of the first tile on the device and with every CU at work
     double epilogue;                             // us a round
@@ -646,12 +651,17 @@ hipError_t launch_typed(const Mx4Product &p, hipStream_t stream) {
     if (EPI == kLinear) offer(12, 64, 128, {0.5, 0.95, 1.0, 2});
     else offer(12, 64, 64, {0.5, 0.55, 1.0, 1});
     offer(22, 128, 2 * W, {0.55, 1.2, 1.5, 2});
+    if (EPI == kLinear) offer(23, 128, 192, {0.7, 0.87, 2.3, 1});
+    if (EPI == kLinear) offer(33, 192, 192, {0.85, 1.18, 2.8, 1});
     offer(34, 192, 4 * W, {1.02, 1.42, 3.0, 1});
     offer(44, 256, 4 * W, {1.18, 1.73, 4.0, 1});
+    if constexpr (EPI == kLinear) {
+        if (best == 11) return launch_tile<EPI, BF16, 1, 1, 4>(p, stream);
+        if (best == 23) return launch_tile<EPI, BF16, 2, 3, 2>(p, stream);
+        if (best == 33) return launch_tile<EPI, BF16, 3, 3, 2>(p, stream);
+    }
     switch (best) {
         case 0: return launch_rows<EPI, BF16, 2>(p, cus, stream);
-        case 11:
-            if constexpr (EPI == kLinear) return launch_tile<EPI, BF16, 1, 1, 4>(p, stream);
         case 12: return launch_tile<EPI, BF16, 1, 2, EPI == kLinear ? 2 : 4>(p, stream);
         case 22: return launch_tile<EPI, BF16, 2, 2, 2>(p, stream);
         case 34: return launch_tile<EPI, BF16, 3, 4, 2>(p, stream);
