@@ -535,7 +535,8 @@ int p4q_w4a4_linear(int M, int N_out, int K_in,
  *
  * p4q_quant_mx4: codes and scales of x's rows; unless it is NULL, values
  *   [M, ldv] (dt) receives what they stand for, exactly (the fake-quantized
- *   rows).  The same call quantizes weight rows.
+ *   rows; values may be x, with its row stride).  The same call quantizes weight
+ *   rows.
  *
  * p4q_mx4_linear: y[m][n] = round(sum_k A[m][k] W[n][k]) on the numbers that
  *   the codes and scales stand for, fp32 sums in an unspecified order, rounded
@@ -547,6 +548,7 @@ int p4q_w4a4_linear(int M, int N_out, int K_in,
  * p4q_mx4_gated_linear_quant: the same, whose result leaves in MXFP4 instead
  *   (the codes of the fp32 products), ready for the next p4q_mx4_linear;
  *   N_out % 32 == 0.
+ * The results of products must not overlap their operands.
  *
  * p4q_residual_rmsnorm_quant: what lies between two blocks of a decoder layer.
  *   r' = post_gamma ? r / rms(r) * post_gamma : r    (the block's output)
@@ -562,8 +564,10 @@ int p4q_w4a4_linear(int M, int N_out, int K_in,
  *   stride); other overlaps are not allowed.  gamma, post_gamma and gate are
  *   [d] of dt.
  *
- * Results do not depend on anything but a row's own values (and, of products,
- *   on M and the sizes through the order of the fp32 sums).  No workspace.
+ * A row's results depend on that row alone (and, of products, on the weight, and
+ *   in the last bits of the fp32 sums on M, whose size picks the kernel), not on
+ *   the order in which parts of a call finish.  No workspace; nothing is kept
+ *   between calls.
  * Limits: M >= 1; 32 <= K <= 131072 (products, quantizer), d <= 16384;
  *   quantizer: M ceil(K / 512) < 2^26; norm: M < 2^23; products: M <= 2^20,
  *   1 <= N_out <= 2^22; row strides of 16-bit operands >= the row, of x, r,

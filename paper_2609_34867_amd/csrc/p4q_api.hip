@@ -546,6 +546,8 @@ int p4q_quant_mx4(p4q_dtype dt, int M, int K, const void *x, int64_t ldx, uint8_
     if (!rows_ok(x, ldx, K) || (values && !rows_ok(values, ldv, K)))
         return fail(P4Q_ERR_INVALID_ARG, "p4q_quant_mx4: ldx=%lld ldv=%lld (need >= K, multiples of 8; 16-byte aligned rows)",
                     (long long)ldx, (long long)ldv);
+    if (values == x && ldv != ldx)
+        return fail(P4Q_ERR_INVALID_ARG, "p4q_quant_mx4: values in place need the same row stride");
     if (!aligned(codes, 16) || !aligned(scales, 16)) return fail(P4Q_ERR_INVALID_ARG, "p4q_quant_mx4: misaligned pointer");
     return hip_status(p4q::launch_quant_mx4(dt, M, K, x, ldx, codes, scales, values, ldv, stream), "p4q_quant_mx4");
 }
@@ -608,6 +610,8 @@ int p4q_mx4_gated_linear_quant(int M, int N_out, int K, const uint8_t *a_codes,
     if (N_out % 32 != 0) return fail(P4Q_ERR_INVALID_ARG, "%s: N_out=%d not a multiple of 32", who, N_out);
     if (!codes || !scales || !aligned(codes, 16) || !aligned(scales, 16))
         return fail(P4Q_ERR_INVALID_ARG, "%s: codes or scales null or misaligned", who);
+    if (codes == a_codes || scales == a_scales)
+        return fail(P4Q_ERR_INVALID_ARG, "%s: the result cannot replace the activations", who);
     p4q::Mx4Product p = mx4_product(M, N_out, K, a_codes, a_scales, w_codes, w_scales);
     p.codes = codes, p.scales = scales;
     return hip_status(p4q::launch_mx4_gated(P4Q_BF16, p, stream), who);

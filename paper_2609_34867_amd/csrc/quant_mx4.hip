@@ -5,7 +5,7 @@
 // scale bytes that a row's padding comes in.  Behind the row's end the lanes
 // hold zeros, whose scale byte is the padding's 0.  One pass over memory: 2
 // bytes of a value read, 17/32 written, and 2 more where the fake-quantized
-// values are asked for.
+// values are asked for (a lane's own 16 bytes, so they may replace x).
 #include "mx4_device.h"
 #include "p4q_internal.h"
 #include "q4_device.h"
@@ -16,10 +16,10 @@ namespace {
 constexpr int kThreads = 256;
 
 template <bool BF16>
-__global__ __launch_bounds__(kThreads) void k_quant_mx4(const uint8_t *__restrict__ x, int64_t ldx_bytes,
+__global__ __launch_bounds__(kThreads) void k_quant_mx4(const uint8_t *x, int64_t ldx_bytes,
                                                         int64_t items, int groups, int chunks,
                                                         uint8_t *__restrict__ codes, uint8_t *__restrict__ scales,
-                                                        uint8_t *__restrict__ values, int64_t ldv_bytes) {
+                                                        uint8_t *values, int64_t ldv_bytes) {
     const int lane = threadIdx.x & 63;
     const int64_t item = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
     if (item >= items) return;

@@ -39,7 +39,7 @@ def gated(**kw):
 
 
 def gated_quant(**kw):
-    return call("p4q_mx4_gated_linear_quant", dict(M=4, N=32, K=64, ac=P, sa=P, wc=P, sw=P, codes=P, scales=P), kw)
+    return call("p4q_mx4_gated_linear_quant", dict(M=4, N=32, K=64, ac=P, sa=P, wc=P, sw=P, codes=2 * P, scales=2 * P), kw)
 
 
 def norm(**kw):
@@ -58,7 +58,8 @@ def refused(fn, kw, status):
     (dict(K=131104, ldx=131104), UNSUPPORTED), (dict(M=1 << 26), UNSUPPORTED), (dict(M=1 << 25, K=1024, ldx=1024), UNSUPPORTED),
     (dict(x=None), BAD), (dict(codes=None), BAD), (dict(scales=None), BAD), (dict(x=P + 8), BAD), (dict(ldx=56), BAD),
     (dict(ldx=68), BAD), (dict(codes=P + 4), BAD), (dict(scales=P + 8), BAD), (dict(values=P, ldv=56), BAD),
-    (dict(values=P, ldv=65), BAD), (dict(values=P + 2, ldv=64), BAD)])
+    (dict(values=P, ldv=65), BAD), (dict(values=P + 2, ldv=64), BAD),
+    (dict(values=P, ldv=72), BAD)])
 def test_quant_refusals(kw, status):
     refused(quant, kw, status)
 
@@ -78,7 +79,7 @@ def test_product_refusals(fn, kw, status):
 
 @pytest.mark.parametrize("kw,status", [(k, s) for k, s in [({a: b for a, b in kw.items() if a != "ldy"}, s) for kw, s in PRODUCT]] + [
     (dict(N=8), BAD), (dict(N=48), BAD), (dict(codes=None), BAD), (dict(scales=None), BAD), (dict(codes=P + 8), BAD),
-    (dict(scales=P + 8), BAD)])
+    (dict(scales=P + 8), BAD), (dict(codes=P), BAD), (dict(scales=P), BAD)])
 def test_gated_quant_refusals(kw, status):
     refused(gated_quant, kw, status)
 

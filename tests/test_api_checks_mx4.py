@@ -98,3 +98,72 @@ def test_gated_checks():
     raises("disagree on K", fn, C, S, u8(128, 32), sw)
     raises("codes must have shape", fn, C, S, w, sw, u8(6, 64))
     raises("scales must have shape", fn, C, S, w, sw, u8(6, 32), u8(6, 2))
+
+
+# ------------------------------------------------------------------ another device than the current one
+class Recorder:
+    """Stands in for the library: keeps what each call is given."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        def call(*a):
+            self.calls.append((name, a))
+            return 0
+        return call
+
+
+def test_calls_on_another_device_pass_everything_on(monkeypatch):
+    """Tensors of a device that is not current: the call is made again, with that
+    device current and the same arguments."""
+    from contextlib import contextmanager
+    rec, entered = Recorder(), []
+
+    @contextmanager
+    def device(d):
+        entered.append(d)
+        yield
+
+    monkeypatch.setattr(api, "lib", lambda: rec)
+    monkeypatch.setattr(api, "_stream", lambda d: 7)
+    monkeypatch.setattr(api.torch.cuda, "device", device)
+    h, v = f16(6, 96), f16(6, 96)
+    w, sw = u8(128, 48), u8(128, 16)
+    calls = [
+        lambda: api.quant_mx4(X, C, S, v),
+        lambda: api.residual_rmsnorm_quant(X, G, h, 1e-3, "int4", 0.5, G, G, 0.25, h, C, torch.zeros(6), v),
+        lambda: api.residual_rmsnorm_quant(X, G),
+        lambda: api.mx4_linear(C, S, W, SW, torch.float16),
+        lambda: api.mx4_linear(C, S, W, SW, y=f16(6, 10)),
+        lambda: api.mx4_gated_linear(C, S, W, SW, torch.float16),
+        lambda: api.mx4_gated_linear_quant(C, S, w, sw, u8(6, 32), u8(6, 16)),
+    ]
+    for call in calls:
+        got = []
+        for away in (False, True):
+            answers = [away, False]                       # not current, then current
+            monkeypatch.setattr(api, "_elsewhere", lambda *t: answers.pop(0))
+            rec.calls.clear()
+            entered.clear()
+            call()
+            assert entered == ([torch.device("cpu")] if away else [])
+            # (addresses of the tensors made in each call differ)
+            got.append([(n, [x for x in a if not (isinstance(x, int) and x > 1 << 20)]) for n, a in rec.calls])
+        assert got[0] == got[1] and len(got[0]) == 1
+
+
+def test_new_outputs(monkeypatch):
+    monkeypatch.setattr(api, "lib", lambda: Recorder())
+    monkeypatch.setattr(api, "_stream", lambda d: 7)
+    monkeypatch.setattr(api, "_elsewhere", lambda *t: False)
+    said = lambda *ts: [(tuple(t.shape), t.dtype) for t in ts]  # noqa: E731
+    held = [((6, 48), torch.uint8), ((6, 16), torch.uint8)]
+    assert said(*api.quant_mx4(X)) == held
+    codes, scales, h = api.residual_rmsnorm_quant(X, G)
+    assert said(codes, scales) == held and h is X
+    codes, scales, h = api.residual_rmsnorm_quant(X, G, X, fmt="int4")
+    assert said(codes, scales, h) == [held[0], ((6,), torch.float32), ((6, 96), torch.float16)]
+    assert said(api.mx4_linear(C, S, W, SW)) == [((6, 10), torch.bfloat16)]
+    assert said(api.mx4_gated_linear(C, S, W, SW, torch.float16)) == [((6, 5), torch.float16)]
+    assert said(*api.mx4_gated_linear_quant(C, S, u8(128, 48), u8(128, 16))) == [((6, 32), torch.uint8), ((6, 16), torch.uint8)]

@@ -81,6 +81,19 @@ def test_quant_sizes(M, K):
     check_quant(rows(M + K, M, K, "bf16"), "bf16")
 
 
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+def test_quant_values_in_place(dtype):
+    x = rows(12, 50, 1056, dtype)
+    t = to_gpu(x, dtype)
+    codes, scales = p4q.quant_mx4(t, values=t)
+    rc, rs = oracle.quant_mx4(f64(x, dtype))
+    assert np.array_equal(to_np(codes), rc) and np.array_equal(to_np(scales), rs)
+    assert np.array_equal(f64(to_np(t), dtype), oracle.mx4_values(rc, rs))
+    # what is on the grid stays
+    again = p4q.quant_mx4(t)
+    assert np.array_equal(oracle.mx4_values(*(to_np(z) for z in again)), oracle.mx4_values(rc, rs))
+
+
 def test_quant_row_gaps():
     check_quant(rows(2, 9, 96), "fp16", ldx=104, ldv=128)
     check_quant(rows(3, 33, 1056), "fp16", ldx=1064, ldv=1056)
@@ -215,7 +228,10 @@ def fp32_sums(K):
 SIZES = [(1, 1, 32), (1, 33, 64), (3, 5, 96), (16, 32, 256), (17, 31, 288), (31, 65, 480), (32, 64, 512), (33, 100, 1056),
          (64, 256, 4096), (65, 129, 544), (128, 128, 1024), (130, 257, 1120), (257, 300, 320), (300, 520, 1568),
          (1, 4096, 4096), (5, 1000, 5120), (513, 768, 768), (1025, 1031, 1056), (2049, 2080, 512),
-         (4100, 4200, 96), (3000, 6200, 1184), (16400, 1030, 288)]
+         (4100, 4200, 96), (3000, 6200, 1184), (16400, 1030, 288),
+         # where each size of tile is taken, with rows, columns and k past the last whole one
+         (1300, 67, 96), (1290, 61, 1312), (130, 6211, 96), (4100, 1050, 800), (4090, 1056, 1056), (1300, 6211, 288),
+         (1000, 8219, 96), (1000, 8224, 1056), (4100, 3003, 288), (4097, 3000, 1056)]
 
 
 @pytest.mark.parametrize("M,N,K", SIZES)
@@ -236,7 +252,8 @@ def check_product(y, ref, mag, K, dtype):
     assert (err <= tol).all(), f"{(err > tol).sum()} values, worst {np.max(err / tol)}"
 
 
-@pytest.mark.parametrize("M,N,K", [(1, 77, 13824), (4, 160, 131072), (16, 96, 11008), (200, 160, 4096), (700, 260, 2080)])
+@pytest.mark.parametrize("M,N,K", [(1, 77, 13824), (4, 160, 131072), (16, 96, 11008), (200, 160, 4096), (700, 260, 2080),
+                                   (1100, 40, 32768)])
 def test_linear_rounding(M, N, K):
     x, w = rows(M, M, K, "bf16"), rows(N, N, K, "bf16")
     a, b = oracle.quant_mx4(f64(x, "bf16")), oracle.quant_mx4(f64(w, "bf16") * 2.0 ** -6)
@@ -291,7 +308,8 @@ def gated_reference(a, w, N, K, exact):
 
 GATED = [(1, 32, 32), (1, 33, 64), (7, 1, 96), (16, 64, 1056), (33, 100, 288), (40, 352, 4096), (130, 129, 320), (300, 260, 544),
          (520, 512, 512), (1030, 1056, 288), (2050, 1030, 256),
-         (4100, 2112, 96), (2900, 3011, 544)]
+         (4100, 2112, 96), (2900, 3011, 544), (1300, 64, 96), (1290, 61, 1056), (390, 8224, 96), (1000, 4128, 1056),
+         (700, 8219, 288), (700, 8224, 1056)]
 
 
 @pytest.mark.parametrize("M,N,K", GATED)
@@ -306,6 +324,46 @@ def test_gated(M, N, K):
         err = np.abs(f64(to_np(y), dtype) - ref)
         lim = tol + HALF[dtype] * (np.abs(ref) + tol) + TINY[dtype]
         assert (err <= lim).all(), f"{dtype}: {(err > lim).sum()} values, worst {np.max(err / lim)}"
+
+
+@pytest.mark.parametrize("M", [2, 30, 200, 1300, 4100])
+def test_gated_nan_blocks(M):
+    """A NaN block of a row makes that row NaN; one of a gate or an up row, its output;
+    quantized, every block that one of them enters."""
+    N, K = 224, 320
+    a, w = operand(8, M, K, 123, 125), operand(9, 2 * N, K, 121, 123)
+    clean, held = (p4q.mx4_gated_linear(*gpu(a), *gpu(w)), p4q.mx4_gated_linear_quant(*gpu(a), *gpu(w)))
+    a[1][M - 1, 9], w[1][3, 0], w[1][N + 40, 5] = 255, 255, 255
+    nan = np.zeros((M, N), bool)
+    nan[M - 1], nan[:, 3], nan[:, 40] = True, True, True
+    y = to_np(p4q.mx4_gated_linear(*gpu(a), *gpu(w)))
+    assert np.array_equal(np.isnan(f64(y, "bf16")), nan)
+    assert np.array_equal(y[~nan], to_np(clean)[~nan])
+    codes, scales = (to_np(t) for t in p4q.mx4_gated_linear_quant(*gpu(a), *gpu(w)))
+    blocks = nan.reshape(M, -1, 32).any(2)
+    assert np.array_equal(scales[:, :N // 32] == 255, blocks)
+    assert (codes.reshape(M, -1, 16)[blocks] == 0).all() and (scales[:, N // 32:] == 0).all()
+    assert np.array_equal(codes.reshape(M, -1, 16)[~blocks], to_np(held[0]).reshape(M, -1, 16)[~blocks])
+    assert np.array_equal(scales[:, :N // 32][~blocks], to_np(held[1])[:, :N // 32][~blocks])
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+def test_gated_far_gates(dtype):
+    """Gates from far below zero, where SiLU vanishes, to far above, where it is the
+    gate: no infinity or NaN where the product has none."""
+    K, N = 32, 96
+    ac, sa = np.zeros((40, 16), np.uint8), np.zeros((40, 16), np.uint8)
+    wc, sw = np.zeros((2 * N, 16), np.uint8), np.zeros((2 * N, 16), np.uint8)
+    ac[:, 0], sa[:, 0] = 0x02, 127                          # 1, 0, 0, ...
+    wc[:, 0], sw[:, 0] = 0x02, 127
+    wc[:N // 2, 0] = 0x0A                                   # half of the gates are negative
+    sw[:N, 0] = 127 + np.tile(np.arange(-24, 24), 2)        # +- 2^-24 .. 2^23
+    sw[N:, 0] = 127 - 9
+    a, w = (ac, sa), (wc, sw)
+    ref, tol = gated_reference(a, w, N, K, exact=True)
+    y = f64(to_np(p4q.mx4_gated_linear(*gpu(a), *gpu(w), out_dtype=TORCH[dtype])), dtype)
+    assert np.isfinite(y).all()
+    assert (np.abs(y - ref) <= tol + HALF[dtype] * (np.abs(ref) + tol) + TINY[dtype]).all()
 
 
 def check_nearest(codes, scales, ref, tol):
@@ -329,7 +387,7 @@ def check_nearest(codes, scales, ref, tol):
     assert (np.abs(v - ref) <= best + 2 * tol).all(), "codes"
 
 
-@pytest.mark.parametrize("M,N,K", [c for c in GATED if c[1] % 32 == 0] + [(3, 544, 96), (65, 1056, 512), (1000, 4128, 64)])
+@pytest.mark.parametrize("M,N,K", [c for c in GATED if c[1] % 32 == 0] + [(3, 544, 96), (65, 1056, 512), (1000, 4128, 64), (900, 4224, 288)])
 def test_gated_quant(M, N, K):
     a, w = operand(M, M, K, 123, 125), operand(N, 2 * N, K, 121, 123)
     ref, tol = gated_reference(a, w, N, K, exact=True)
@@ -400,3 +458,57 @@ def test_captured_and_replayed(M):
         eh, emid, ey = mlp(*inputs[i], gamma, w1, w2)
         assert torch.equal(h, eh) and torch.equal(y, ey)
         assert all(torch.equal(a, b) for a, b in zip(mid, emid))
+
+
+def test_another_stream():
+    """Calls go to the current stream: on a side stream they wait for what was queued
+    there."""
+    M, d, f = 200, 544, 512
+    w1, w2 = (gpu(w) for w in mlp_weights(d, f, 13))
+    gamma = to_gpu(store(np.ones(d), "fp16"))
+    x, r = to_gpu(rows(40, M, d, "fp16", 1.0)), to_gpu(rows(41, M, d, "fp16", 1.0))
+    h, mid, y = mlp(x, r, gamma, w1, w2)
+    late = torch.zeros_like(x)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        big = torch.randn(4096, 4096, device=dev())
+        for _ in range(10):
+            big = torch.mm(big, big).clamp(-1, 1)
+        late.copy_(x)
+        h2, mid2, y2 = mlp(late, r, gamma, w1, w2)
+    side.synchronize()
+    assert torch.equal(h, h2) and torch.equal(y, y2) and all(torch.equal(a, b) for a, b in zip(mid, mid2))
+
+
+def test_two_streams_at_once():
+    """Nothing is shared between calls."""
+    M, N, K = 600, 1030, 1056
+    ops = [(gpu(operand(50 + i, M, K)), gpu(operand(60 + i, N, K))) for i in range(2)]
+    ref = [p4q.mx4_linear(*a, *w) for a, w in ops]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in range(2)], [[], []]
+    for _ in range(20):
+        for i, st in enumerate(streams):
+            with torch.cuda.stream(st):
+                got[i].append(p4q.mx4_linear(*ops[i][0], *ops[i][1]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(y, ref[i]) for y in got[i])
+
+
+def test_refusals_enqueue_nothing():
+    x = torch.full((4, 64), 3.0, dtype=torch.float16, device=dev())
+    codes, scales = torch.full((4, 32), 9, dtype=torch.uint8, device=dev()), torch.full((4, 16), 9, dtype=torch.uint8, device=dev())
+    with pytest.raises(p4q.P4QError, match="K=0|multiple of 32"):
+        p4q.quant_mx4(x[:, :48], codes=codes[:, :24].contiguous(), scales=scales)
+    with pytest.raises(p4q.P4QError, match="16-byte aligned rows"):
+        p4q.quant_mx4(torch.zeros(4, 72, dtype=torch.float16, device=dev())[:, 4:68], codes=codes, scales=scales)
+    with pytest.raises(p4q.P4QError, match="cannot replace"):
+        p4q.mx4_gated_linear_quant(codes, scales, *(torch.zeros(128, n, dtype=torch.uint8, device=dev()) for n in (32, 16)), codes=codes)
+    with pytest.raises(p4q.P4QError, match="M=0"):
+        p4q.quant_mx4(x[:0])
+    with pytest.raises(p4q.P4QError, match="clip"):
+        p4q.residual_rmsnorm_quant(x, x[0], clip=0.5, codes=codes, scales=scales)
+    torch.cuda.synchronize()
+    assert bool((codes == 9).all()) and bool((scales == 9).all())
