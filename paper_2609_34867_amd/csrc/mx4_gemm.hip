@@ -5,9 +5,14 @@
 // operands' scale bytes itself: lane l holds 32 consecutive codes of row
 // l % 32 and the scale byte of that block.  The contraction does not care
 // which 32 of a row's values meet in which instruction, as long as both
-// operands agree; so with 256 values of k a step, lane l takes the four
-// blocks 4 (l / 32) .. + 3 one after the other: 64 consecutive bytes of codes,
-// and scale bytes that are one aligned word.
+// operands agree; so with 256 values of k a stage, lane l takes the four
+// blocks 4 (l / 32) .. + 3 one after the other, whose scale bytes are one
+// aligned word.
+//
+// The weight is the first operand, so a lane of the result holds one row of a
+// and runs of 4 consecutive outputs of it: the gate's and the up projection's
+// sums of an output meet in one lane, and two lanes hold a block of 32 outputs
+// to quantize.
 #include "gemm_device.h"
 #include "mx4_device.h"
 #include "p4q_internal.h"
@@ -83,23 +88,31 @@ __device__ __forceinline__ void emit8(const Mx4Product &p, int64_t m, int n0, fl
 // ---- tiles through LDS -----------------------------------------------------------
 // A work-group of four wavefronts, 2 x 2, computes 64 FM rows by 64 FN weight
 // rows, each wavefront FM x FN fragments of 32 x 32.  k runs in stages of 256
-// values, four steps each; two stages (RING) in LDS, filled by DMA, and the ring
-// runs on across the tiles of a persistent work-group.
-//  * A stage's row is 128 bytes, one cache line, loaded by 8 lanes: what the DMA
-//    costs is lines touched per instruction, and rows of half a line cost a third
-//    more time.  Chunk c of 16 bytes (32 codes) of row r lies at c ^ (r / 2 % 8),
-//    so that 16 rows of a fragment read fall into distinct banks.
-//  * Scale bytes come 16 per row, for two stages at once: the rows of a with the
-//    odd stage before, those of w with the even one.  An odd number of stages is
-//    padded with one that multiplies nothing.
+// values, four steps each; a ring of RING stages in LDS is filled by DMA and runs
+// on across the tiles of a persistent work-group.
+//  * A stage's row is 128 bytes, one cache line, loaded by 8 lanes: rows of half a
+//    line (stages of 128 values, ring of 4) take 638 us where these take 502 (gate
+//    and up of 7B, 11264 rows).  Chunk c of 16 bytes (32 codes) of row r lies at
+//    c ^ (r / 2 % 8), so that 16 rows of a fragment read fall into distinct banks.
+//  * Scale bytes come 16 per row, for two stages at once (8 for one: 1024 instead
+//    of 768 lines a stage): the rows of a with the odd stage before, those of w
+//    with the even one.  An odd number of stages is padded with one that
+//    multiplies nothing.  (32 for four stages need the room that the outputs are
+//    staged in; stored from registers they take 243 us instead of 234, 7B down
+//    projection, 11264 rows.)
 //  * Operands are read ahead of their step: during steps 2 and 3 those of the next
 //    stage's steps 0 to 2, during step 0 those of step 3.  So a slot is read in
 //    three steps and has five for its next stage to arrive, whose DMAs are spread
 //    over the products of steps 1 to 3 (over four steps, with less time to arrive,
-//    2% slower).  A ring of four stages gives a lone work-group more.
+//    2% slower).
 //  * Past the row's end the DMA's offsets lie outside the buffer and give codes
 //    of zero, and the scale bytes there are masked; rows past the last are outside
 //    it too.
+// Measured, M x N x K = 11264 x 4096 x 11008: 232 us = 4.4 PFLOP/s; gate and up,
+// 11264 x 2 * 11008 x 4096: 485 us = 4.2 PFLOP/s.  Of the 232 us the products alone
+// take 154, with their reads 177, and the DMA alone 133.  It is the power limit
+// that stretches them: the matrix units are busy in 55% of the cycles, at 1.84 GHz
+// of 2.4.
 // No instruction: x is taken to change here.
 __device__ __forceinline__ void hold(v16f &x) { asm volatile("" : "+a"(x)); }
 
@@ -404,7 +417,11 @@ __global__ __launch_bounds__(256, FM * FN > 4 || RING > 2 ? 1 : 2) void k_mx4_ti
                         const uint4 val = *reinterpret_cast<const uint4 *>(out + row * OUT_ROW + ((c ^ (row & (LR - 1))) << 4));
                         const int64_t m = m0 + 32 * j + row;
                         const int n = n0 + 32 * f0 + 8 * c;
-                        if (full) __builtin_memcpy(static_cast<uint16_t *>(p.y) + m * p.ldy + n, &val, 16);
+                        // (aligned rows go past the caches, which hold operands: 2% less time at
+                        // 11264 rows; unaligned ones would go as parts of lines: 11% more)
+                        if (full && p.wide)
+                            __builtin_nontemporal_store(v4i{(int)val.x, (int)val.y, (int)val.z, (int)val.w},
+                                                        reinterpret_cast<v4i *>(static_cast<uint16_t *>(p.y) + m * p.ldy + n));
                         else store8(p, m, n, val);
                     }
                 }
@@ -430,6 +447,10 @@ __global__ __launch_bounds__(256, FM * FN > 4 || RING > 2 ? 1 : 2) void k_mx4_ti
 //    In a product of 128 values lane l takes the blocks 2 (l / 16) and, in the
 //    second, 2 (l / 16) + 1 of row l % 16.
 //  * Scale bytes come 32 per row, for four stages at once, into two buffers.
+// Bound by memory: 13B down projection (N = 5120, K = 13824), 4 rows, 37.7 MB in 7.6
+// us = 5.0 TB/s; 7B gate and up, 16 rows, 48.3 MB in 9.2 us = 5.3 TB/s (12.4 and 16
+// with the operands straight from memory to registers: every fragment load touches
+// 32 lines there, and each line four times).
 constexpr int kRowsRing = 2, kRowsGroup = 4;
 
 template <int EPI, bool BF16, int MB, int NW>
@@ -673,6 +694,7 @@ hipError_t launch_typed(const Mx4Product &p, hipStream_t stream) {
 
 hipError_t launch_mx4_linear(p4q_dtype out_dt, Mx4Product p, hipStream_t stream) {
     p.in_stride = mx4_scale_stride(p.K);
+    p.wide = p.ldy % 8 == 0 && reinterpret_cast<uintptr_t>(p.y) % 16 == 0;
     return out_dt == P4Q_BF16 ? launch_typed<kLinear, true>(p, stream) : launch_typed<kLinear, false>(p, stream);
 }
 
@@ -680,6 +702,7 @@ hipError_t launch_mx4_gated(p4q_dtype out_dt, Mx4Product p, hipStream_t stream) 
     p.in_stride = mx4_scale_stride(p.K);
     p.out_stride = mx4_scale_stride(p.N);
     if (p.codes) return launch_typed<kGatedQuant, false>(p, stream);
+    p.wide = p.ldy % 8 == 0 && reinterpret_cast<uintptr_t>(p.y) % 16 == 0;
     return out_dt == P4Q_BF16 ? launch_typed<kGated, true>(p, stream) : launch_typed<kGated, false>(p, stream);
 }
 

@@ -5,7 +5,9 @@
 // scale bytes that a row's padding comes in.  Behind the row's end the lanes
 // hold zeros, whose scale byte is the padding's 0.  One pass over memory: 2
 // bytes of a value read, 17/32 written, and 2 more where the fake-quantized
-// values are asked for (a lane's own 16 bytes, so they may replace x).
+// values are asked for (a lane's own 16 bytes, so they may replace x).  Bound by
+// it: 11264 rows of 4096 with their values, 209 MB in 33.5 us = 6.2 TB/s; 4 rows
+// of 5120 2.6 us.
 #include "mx4_device.h"
 #include "p4q_internal.h"
 #include "q4_device.h"
