@@ -113,8 +113,16 @@ __device__ __forceinline__ void emit8(const Mx4Product &p, int64_t m, int n0, fl
 // take 154, with their reads 177, and the DMA alone 133.  It is the power limit
 // that stretches them: the matrix units are busy in 55% of the cycles, at 1.84 GHz
 // of 2.4.
-// No instruction: x is taken to change here.
-__device__ __forceinline__ void hold(v16f &x) { asm volatile("" : "+a"(x)); }
+// The sums of a fragment out of the accumulation registers, here and not earlier (left
+// to itself the compiler reads them all before the first pass and spills).  It knows
+// no hazard of these reads: the caller keeps the distance to the last product.
+__device__ __forceinline__ void read_sums(const v16f &acc, float (&v)[16]) {
+#pragma unroll
+    for (int x = 0; x < 16; ++x) {
+        const float a = acc[x];
+        asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v[x]) : "a"(a));
+    }
+}
 
 template <class F, int... I>
 __device__ __forceinline__ void unrolled_seq(F &&f, std::integer_sequence<int, I...>) {
@@ -364,6 +372,8 @@ __global__ __launch_bounds__(256, FM * FN > 4 || RING > 2 ? 1 : 2) void k_mx4_ti
 
         // ---- lane l holds row l % 32 of a fragment, outputs 8 g + 4 (l / 32) + 0..3 in
         // registers 4 g ..
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");   // the last products before the reads of their sums
         int tm, tn;
         tile_at(ck, tm, tn);
         const int64_t m0 = (int64_t)tm * BM + wm * 32 * FM;
@@ -374,20 +384,22 @@ __global__ __launch_bounds__(256, FM * FN > 4 || RING > 2 ? 1 : 2) void k_mx4_ti
         for (int j = 0; j < FM; ++j) {
 #pragma unroll
             for (int f0 = 0; f0 < FO; f0 += EW) {
-                // (opaque here, so that no later pass's sums are read before their turn)
+                float v[EW][16];
 #pragma unroll
                 for (int e = 0; e < EW; ++e) {
-                    hold(acc[f0 + e][j]);
-                    if constexpr (EPI != kLinear) hold(acc[f0 + e + FO][j]);
+                    read_sums(acc[f0 + e][j], v[e]);
+                    if constexpr (EPI != kLinear) {
+                        float u[16];
+                        read_sums(acc[(f0 + e + FO) % FN][j], u);
+#pragma unroll
+                        for (int x = 0; x < 16; ++x) v[e][x] = silu(v[e][x]) * u[x];
+                    }
                 }
                 if constexpr (EPI == kGatedQuant) {
 #pragma unroll
                     for (int e = 0; e < EW; ++e) {
-                        float v[16];
-#pragma unroll
-                        for (int x = 0; x < 16; ++x) v[x] = silu(acc[f0 + e][j][x]) * acc[f0 + e + FO][j][x];
                         uint32_t byte;
-                        const uint2 c = mx4_quantize_halves(v, byte);
+                        const uint2 c = mx4_quantize_halves(v[e], byte);
                         const int64_t m = m0 + 32 * j + r;
                         const int n = n0 + 32 * (f0 + e);
                         if (m < p.M && n < p.N) {
@@ -400,12 +412,7 @@ __global__ __launch_bounds__(256, FM * FN > 4 || RING > 2 ? 1 : 2) void k_mx4_ti
                     for (int e = 0; e < EW; ++e)
 #pragma unroll
                         for (int g = 0; g < 4; ++g) {
-                            float o[4];
-#pragma unroll
-                            for (int x = 0; x < 4; ++x) {
-                                o[x] = acc[f0 + e][j][4 * g + x];
-                                if constexpr (EPI == kGated) o[x] = silu(o[x]) * acc[(f0 + e + FO) % FN][j][4 * g + x];
-                            }
+                            const float *o = v[e] + 4 * g;
                             const int chunk = (4 * e + g) ^ (r & (4 * EW - 1));
                             *reinterpret_cast<uint2 *>(out + r * OUT_ROW + chunk * 16 + 8 * h) =
                                 make_uint2(round16x2<BF16>(o[0], o[1]), round16x2<BF16>(o[2], o[3]));
