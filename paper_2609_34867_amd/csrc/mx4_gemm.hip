@@ -108,8 +108,8 @@ __device__ __forceinline__ void emit8(const Mx4Product &p, int64_t m, int n0, fl
 //  * Past the row's end the DMA's offsets lie outside the buffer and give codes
 //    of zero, and the scale bytes there are masked; rows past the last are outside
 //    it too.
-// Measured, M x N x K = 11264 x 4096 x 11008: 232 us = 4.4 PFLOP/s; gate and up,
-// 11264 x 2 * 11008 x 4096: 485 us = 4.2 PFLOP/s.  Of the 232 us the products alone
+// Measured, M x N x K = 11264 x 4096 x 11008: 230 us = 4.4 PFLOP/s; gate and up,
+// 11264 x 2 * 11008 x 4096: 482 us = 4.2 PFLOP/s.  Of the 230 us the products alone
 // take 154, with their reads 177, and the DMA alone 133.  It is the power limit
 // that stretches them: the matrix units are busy in 55% of the cycles, at 1.84 GHz
 // of 2.4.
