@@ -105,6 +105,11 @@ __device__ __forceinline__ void emit8(const Mx4Product &p, int64_t m, int n0, fl
 //    three steps and has five for its next stage to arrive, whose DMAs are spread
 //    over the products of steps 1 to 3 (over four steps, with less time to arrive,
 //    2% slower).
+//  * KS = 2: two parts of the work-group, of four wavefronts and a ring each, take a
+//    half of k each for the same tile, one tile per work-group, and add their sums in
+//    LDS.  For long rows and fewer tiles than CUs, where one wavefront per SIMD waits
+//    for its barriers and reads: 128 x 5120 x 13824 by 64 x 64 24.7 -> 20.6 us, 292 x
+//    5120 x 13824 by 64 x 128 30.3 -> 26.1 (four parts no faster: 20.4).
 //  * Past the row's end the DMA's offsets lie outside the buffer and give codes
 //    of zero, and the scale bytes there are masked; rows past the last are outside
 //    it too.
@@ -134,11 +139,50 @@ __device__ __forceinline__ void unrolled(F &&f) {
     unrolled_seq(f, std::make_integer_sequence<int, N>{});
 }
 
+// A tile whose k is shared by KS parts of a work-group: the sums of its parts, added in
+// LDS in their order, and its outputs
+template <bool BF16, int FM, int FN, int KS>
+__device__ __forceinline__ void add_parts(const Mx4Product &p, uint8_t *smem, int wave, int lane,
+                                          const v16f (&acc)[FN][FM], int64_t m0, int n0) {
+    constexpr int X = FM * FN;
+    float4 *red = reinterpret_cast<float4 *>(smem);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // no DMA into LDS from here on
+    __syncthreads();
+    // [part][wavefront][fragment][registers 4 g ..][lane], lanes exchanged so that the
+    // threads of a quad below read from different banks
+    unrolled<X>([&](auto x_c) __attribute__((always_inline)) {
+        constexpr int x = decltype(x_c)::value, f = x / FM, j = x % FM;
+        float v[16];
+        read_sums(acc[f][j], v);
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+            red[((wave * X + x) * 4 + g) * 64 + (lane ^ (4 * g))] = make_float4(v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]);
+    });
+    __syncthreads();
+    // a quad of threads has 32 outputs of a row, 8 each
+    for (int t = (int)threadIdx.x; t < 64 * FM * 2 * FN * 4; t += 256 * KS) {
+        const int g = t & 3, row = (t >> 2) % (64 * FM), q = (t >> 2) / (64 * FM);
+        const int wn = q / FN, f = q % FN, wm = row / (32 * FM), j = row / 32 % FM, r = row & 31;
+        float v[8] = {};
+#pragma unroll
+        for (int k = 0; k < KS; ++k)
+#pragma unroll
+            for (int hh = 0; hh < 2; ++hh) {
+                const float4 s = red[(((k * 4 + wn * 2 + wm) * X + f * FM + j) * 4 + g) * 64 + ((r + 32 * hh) ^ (4 * g))];
+                v[4 * hh + 0] += s.x;
+                v[4 * hh + 1] += s.y;
+                v[4 * hh + 2] += s.z;
+                v[4 * hh + 3] += s.w;
+            }
+        store8(p, m0 + row, n0 + 32 * q + 8 * g, round16x8<BF16>(v));
+    }
+}
+
 constexpr int kRowBytes = 128;                   // codes of a row in a stage
 constexpr int kRowScales = 16;                   // scale bytes of a row, two stages'
 
-template <int EPI, bool BF16, int FM, int FN, int RING>
-__global__ __launch_bounds__(256, FM * FN > 4 || RING > 2 ? 1 : 2) void k_mx4_tile(const Mx4Product p, int tiles_m, int tiles_n) {
+template <int EPI, bool BF16, int FM, int FN, int RING, int KS = 1>
+__global__ __launch_bounds__(256 * KS, FM * FN > 4 || RING > 2 || KS > 1 ? 1 : 2) void k_mx4_tile(const Mx4Product p, int tiles_m, int tiles_n) {
     constexpr int BM = 64 * FM, BW = 64 * FN;              // rows of a, of w
     constexpr int BN = EPI == kLinear ? BW : BW / 2;       // outputs: half of w's rows are the gate's
     constexpr int FO = EPI == kLinear ? FN : FN / 2;       // fragments of outputs per wavefront
@@ -146,17 +190,23 @@ __global__ __launch_bounds__(256, FM * FN > 4 || RING > 2 ? 1 : 2) void k_mx4_ti
     constexpr int OFF_SCALES = RING * STAGE, OFF_SW = BM * kRowScales, SCALES = OFF_SW + BW * kRowScales;
     constexpr int S_RING = RING / 2 + 1, OFF_OUT = OFF_SCALES + S_RING * SCALES;
     constexpr int EW = FO >= 2 && FM * FN >= 16 ? 2 : 1;   // fragments stored together
-    constexpr int OUT_ROW = 64 * EW, OUT_WAVE = EPI == kGatedQuant ? 0 : 32 * OUT_ROW;
+    constexpr int OUT_ROW = 64 * EW, OUT_WAVE = EPI == kGatedQuant || KS > 1 ? 0 : 32 * OUT_ROW;
     constexpr int CODE_DMAS = 2 * (FM + FN), DMAS = CODE_DMAS + 1;
     static_assert(EPI == kLinear || FN % 2 == 0, "gate and up fragments");
     static_assert(RING % 2 == 0, "scales of two stages");
     static_assert(FM <= 4 && FN <= 4, "a wavefront's share of the scales is one load");
-    __shared__ __attribute__((aligned(1024))) uint8_t smem[OFF_OUT + 4 * OUT_WAVE];
+    static_assert(KS == 1 || (EPI == kLinear && FM * FN * 16384 <= OFF_OUT), "the parts' sums lie where their stages did");
+    __shared__ __attribute__((aligned(1024))) uint8_t smem_all[KS * OFF_OUT + 4 * OUT_WAVE];
 
     const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
-    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int wave_all = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int wave = wave_all & 3, part = KS > 1 ? wave_all >> 2 : 0;
     const int wm = wave & 1, wn = wave >> 1;
-    const int blocks = p.K / 32, KT = (blocks + 7) / 8, KT2 = (KT + 1) & ~1;
+    uint8_t *smem = smem_all + part * OFF_OUT;
+    const int blocks = p.K / 32;
+    // this part's stages: KT of them, from the one at k0; an even number, so that scale bytes start 16 bytes apart
+    const int KT_all = (blocks + 7) / 8, KT2 = ((KT_all + KS - 1) / KS + 1) & ~1;
+    const int KT = KS > 1 ? KT2 : KT_all, k0 = part * KT2;
     const uint32_t kb = (uint32_t)p.K / 2, sb = (uint32_t)p.in_stride;
 
     // this work-group's tiles: a contiguous share of its XCD's range
@@ -219,7 +269,7 @@ __global__ __launch_bounds__(256, FM * FN > 4 || RING > 2 ? 1 : 2) void k_mx4_ti
         iss_lds = lds + (uint32_t)iss_slot * STAGE;
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-            const uint32_t c = (uint32_t)iss_kt * 8u + c_chunk[x];
+            const uint32_t c = (uint32_t)(k0 + iss_kt) * 8u + c_chunk[x];
             iss_v[x] = c < (uint32_t)blocks ? c_row * kb + c * 16u : kOutside;
         }
     };
@@ -230,12 +280,12 @@ __global__ __launch_bounds__(256, FM * FN > 4 || RING > 2 ? 1 : 2) void k_mx4_ti
             if (iss_kt & 1) {
                 const uint32_t row = (uint32_t)wave * 16 * FM;
                 if (lane < 16 * FM)
-                    dma16(dSA, (row + (uint32_t)lane) * sb + (uint32_t)sc_kt * 8u, base + row * kRowScales);
+                    dma16(dSA, (row + (uint32_t)lane) * sb + (uint32_t)(k0 + sc_kt) * 8u, base + row * kRowScales);
             } else {
                 const uint32_t row = (uint32_t)wave * 16 * FN;
                 const uint32_t from = EPI == kLinear ? row : (uint32_t)(wave & 1) * 16 * FN;
                 if (lane < 16 * FN)
-                    dma16(dSW, (from + (uint32_t)lane) * sb + (uint32_t)iss_kt * 8u, base + OFF_SW + row * kRowScales);
+                    dma16(dSW, (from + (uint32_t)lane) * sb + (uint32_t)(k0 + iss_kt) * 8u, base + OFF_SW + row * kRowScales);
             }
         } else if constexpr (i <= 2 * FM) {                // 8 rows of a
             const uint32_t g = (uint32_t)(wave * 2 * FM + i - 1);
@@ -291,7 +341,7 @@ __global__ __launch_bounds__(256, FM * FN > 4 || RING > 2 ? 1 : 2) void k_mx4_ti
     scales_a();
     if (lane < 16 * FM) {
         const uint32_t row = (uint32_t)wave * 16 * FM;
-        dma16(dSA, (row + (uint32_t)lane) * sb, lds + OFF_SCALES + (uint32_t)sc_slot * SCALES + row * kRowScales);
+        dma16(dSA, (row + (uint32_t)lane) * sb + (uint32_t)k0 * 8u, lds + OFF_SCALES + (uint32_t)sc_slot * SCALES + row * kRowScales);
     }
     unrolled<RING>([&](auto) __attribute__((always_inline)) {
         issue_begin();
@@ -310,7 +360,7 @@ __global__ __launch_bounds__(256, FM * FN > 4 || RING > 2 ? 1 : 2) void k_mx4_ti
         // number to an even one
         auto stage = [&](int kt, auto kind_c) __attribute__((always_inline)) {
             constexpr bool FIRST = decltype(kind_c)::value == 0, LIVE = decltype(kind_c)::value < 2;
-            const int left = blocks - 8 * kt - 4 * h;
+            const int left = blocks - 8 * (k0 + kt) - 4 * h;
             const uint32_t mask = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
 #pragma unroll
             for (int j = 0; j < FM; ++j) sa[j] = ra[j] & mask;
@@ -376,6 +426,10 @@ __global__ __launch_bounds__(256, FM * FN > 4 || RING > 2 ? 1 : 2) void k_mx4_ti
         asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");   // the last products before the reads of their sums
         int tm, tn;
         tile_at(ck, tm, tn);
+        if constexpr (KS > 1) {
+            add_parts<BF16, FM, FN, KS>(p, smem_all, wave_all, lane, acc, (int64_t)tm * BM, tn * BN);
+            break;
+        }
         const int64_t m0 = (int64_t)tm * BM + wm * 32 * FM;
         const int n0 = tn * BN + wn * 32 * FO;
         const bool full = (int64_t)(tm + 1) * BM <= p.M && (int64_t)(tn + 1) * BN <= p.N;
@@ -618,11 +672,12 @@ struct TileCost {
     double idle, busy;                           // us a stage, of the first tile on the device and with every CU at work
     double epilogue;                             // us a round
     int per_cu;                                  // work-groups
+    int parts = 1;                               // that share k
 };
 inline double tile_cost(const Mx4Product &p, int bm, int bn, const TileCost &c, int cus) {
     const int64_t tiles = (((int64_t)p.M + bm - 1) / bm) * (((int64_t)p.N + bn - 1) / bn);
     const int64_t slots = (int64_t)cus * c.per_cu, whole = tiles / slots;
-    const int stages = (p.K / 32 + 7) / 8;
+    const int stages = ((p.K / 32 + 7) / 8 + c.parts - 1) / c.parts;
     double us = 2.5 + (double)whole * (c.epilogue + stages * c.busy);
     if (const int64_t left = tiles % slots) {
         // two on a CU take nearly twice as long as one, whether or not every CU has two
@@ -639,13 +694,14 @@ inline double rows_cost(const Mx4Product &p, int mb, int frags, int outputs) {
 }
 
 // all outputs by tiles of 64 FM x 64 FN (gated: 32 FN)
-template <int EPI, bool BF16, int FM, int FN, int RING>
+template <int EPI, bool BF16, int FM, int FN, int RING, int KS = 1>
 hipError_t launch_tile(const Mx4Product &p, hipStream_t stream) {
     constexpr int BM = 64 * FM, BN = (EPI == kLinear ? 64 : 32) * FN;
     const int tiles_m = (int)(((int64_t)p.M + BM - 1) / BM), tiles_n = (p.N + BN - 1) / BN;
     const int64_t T = (int64_t)tiles_m * tiles_n;
-    const int64_t grid = std::min<int64_t>(T, (int64_t)device_cus() * (FM * FN > 4 || RING > 2 ? 1 : 2));
-    hipLaunchKernelGGL((k_mx4_tile<EPI, BF16, FM, FN, RING>), dim3((unsigned)grid), dim3(256), 0, stream, p, tiles_m, tiles_n);
+    // (parts of k: a tile each, their sums lie where the next one's stages would)
+    const int64_t grid = KS > 1 ? T : std::min<int64_t>(T, (int64_t)device_cus() * (FM * FN > 4 || RING > 2 ? 1 : 2));
+    hipLaunchKernelGGL((k_mx4_tile<EPI, BF16, FM, FN, RING, KS>), dim3((unsigned)grid), dim3(256 * KS), 0, stream, p, tiles_m, tiles_n);
     return hipGetLastError();
 }
 
@@ -676,7 +732,9 @@ hipError_t launch_typed(const Mx4Product &p, hipStream_t stream) {
         if (us < least) least = us, best = which;
     };
     if (EPI == kLinear) offer(11, 64, 64, {0.38, 0.42, 1.0, 1});
-    if (EPI == kLinear) offer(12, 64, 128, {0.5, 0.95, 1.0, 2});
+    if (EPI == kLinear) offer(112, 64, 64, {0.57, 0.70, 2.0, 1, 2});
+    if (EPI == kLinear) offer(122, 64, 128, {0.79, 0.86, 1.5, 1, 2});
+    if (EPI == kLinear) offer(12, 64, 128, {0.54, 0.95, 1.0, 2});
     else offer(12, 64, 64, {0.5, 0.55, 1.0, 1});
     offer(22, 128, 2 * W, {0.55, 1.2, 1.5, 2});
     if (EPI == kLinear) offer(23, 128, 192, {0.7, 0.87, 2.3, 1});
@@ -685,6 +743,8 @@ hipError_t launch_typed(const Mx4Product &p, hipStream_t stream) {
     offer(44, 256, 4 * W, {1.18, 1.73, 4.0, 1});
     if constexpr (EPI == kLinear) {
         if (best == 11) return launch_tile<EPI, BF16, 1, 1, 4>(p, stream);
+        if (best == 112) return launch_tile<EPI, BF16, 1, 1, 4, 2>(p, stream);
+        if (best == 122) return launch_tile<EPI, BF16, 1, 2, 2, 2>(p, stream);
         if (best == 23) return launch_tile<EPI, BF16, 2, 3, 2>(p, stream);
         if (best == 33) return launch_tile<EPI, BF16, 3, 3, 2>(p, stream);
     }

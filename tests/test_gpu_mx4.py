@@ -231,7 +231,9 @@ SIZES = [(1, 1, 32), (1, 33, 64), (3, 5, 96), (16, 32, 256), (17, 31, 288), (31,
          (4100, 4200, 96), (3000, 6200, 1184), (16400, 1030, 288),
          # where each size of tile is taken, with rows, columns and k past the last whole one
          (1300, 67, 96), (1290, 61, 1312), (130, 6211, 96), (4100, 1050, 800), (4090, 1056, 1056), (1300, 6211, 288),
-         (1000, 8219, 96), (1000, 8224, 1056), (4100, 3003, 288), (4097, 3000, 1056)]
+         (1000, 8219, 96), (1000, 8224, 1056), (4100, 3003, 288), (4097, 3000, 1056),
+         # where two parts of a work-group share k: the second with as many stages, with fewer
+         (1030, 61, 3040), (1030, 61, 5120), (1030, 130, 6176), (200, 4100, 1312), (387, 2500, 3040), (1030, 1001, 1312)]
 
 
 @pytest.mark.parametrize("M,N,K", SIZES)
@@ -285,13 +287,36 @@ def test_linear_nan_and_extreme_scales(M):
     nan[M - 1], nan[:, 5] = True, True
     assert np.array_equal(np.isnan(y), nan)
     assert np.array_equal(y[~nan], f64(store(ref, "fp16"), "fp16")[~nan])
-    # the largest and the smallest bytes against each other
+    # the largest and the smallest bytes against each other, and sums below 2^-126
     (ac, _), (wc, _) = a, w
-    for lo, hi in ((254, 0), (0, 254), (200, 54), (126, 128)):
+    for lo, hi in ((254, 0), (0, 254), (200, 54), (126, 128), (60, 60), (120, 1)):
         sa, sw = np.full_like(a[1], lo), np.full_like(w[1], hi)
         y = p4q.mx4_linear(*gpu((ac, sa)), *gpu((wc, sw)))
         ref = oracle.mx4_linear(ac, sa, wc, sw)[0]
         assert np.array_equal(bits(to_np(y)), bits(store(ref, "bf16"))), (lo, hi)
+
+
+@pytest.mark.parametrize("M,N", [(1030, 200), (387, 2504)])
+def test_linear_shared_k(M, N):
+    """Row gaps, NaN blocks in either part of k, far scales, where two parts share it."""
+    K = 3040
+    a, w = exact_operands(7, M, N, K)
+    ref = oracle.mx4_linear(*a, *w)[0]
+    for ld, first in ((N + 3, 0), (N + 24, 8)):
+        wide = torch.full((M, ld), 7.0, dtype=torch.float16, device=dev())
+        p4q.mx4_linear(*gpu(a), *gpu(w), y=wide[:, first:first + N])
+        assert np.array_equal(bits(to_np(wide[:, first:first + N].contiguous())), bits(store(ref, "fp16"))), (ld, first)
+        assert bool((wide[:, :first] == 7).all()) and bool((wide[:, first + N:] == 7).all())
+    a[1][M - 1, 94], a[1][2, 3], w[1][5, 0], w[1][N - 1, 60] = 255, 255, 255, 255
+    y = f64(to_np(p4q.mx4_linear(*gpu(a), *gpu(w))), "bf16")
+    nan = np.zeros((M, N), bool)
+    nan[[2, M - 1]], nan[:, [5, N - 1]] = True, True
+    assert np.array_equal(np.isnan(y), nan)
+    assert np.array_equal(y[~nan], f64(store(ref, "bf16"), "bf16")[~nan])
+    for lo, hi in ((254, 0), (126, 128)):
+        sa, sw = np.full_like(a[1], lo), np.full_like(w[1], hi)
+        y = p4q.mx4_linear(*gpu((a[0], sa)), *gpu((w[0], sw)))
+        assert np.array_equal(bits(to_np(y)), bits(store(oracle.mx4_linear(a[0], sa, w[0], sw)[0], "bf16"))), (lo, hi)
 
 
 def gated_reference(a, w, N, K, exact):
