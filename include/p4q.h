@@ -554,7 +554,7 @@ int p4q_w4a4_linear(int M, int N_out, int K_in,
  *   r' = post_gamma ? r / rms(r) * post_gamma : r    (the block's output)
  *   h  = round(fl32(x + alpha * gate * r'))           (gate NULL: 1)
  *   P4Q_NORM_INT4: (codes, scales) = those of p4q_rmsnorm_quant(h, gamma, eps,
- *     clip): codes [M, d/2] of Q4, scales fp32 [M];
+ *     clip): codes [M, d/2] of Q4, scales fp32 [M] (as there, for finite h gamma);
  *   P4Q_NORM_MX4: (codes, scales) = MXFP4 of fl32(h * gamma / rms(h)),
  *   rms(z) = sqrt(sum z^2 / d + eps); a row with sum z^2 / d + eps = 0 counts as
  *   zeros.  Everything before a stated rounding is held in 64 bits.  h_out
