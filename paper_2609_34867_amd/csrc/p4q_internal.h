@@ -95,7 +95,7 @@ struct Mx4Product {
     uint8_t *codes, *scales;                         // gated and quantized: instead of y
     // set by the launcher
     int64_t in_stride, out_stride;                   // bytes of a row of scales
-    bool wide;                                       // y's rows are 16-byte aligned
+    bool wide;                                       // y's rows begin at halves of cache lines
 };
 hipError_t launch_mx4_linear(p4q_dtype out_dt, Mx4Product p, hipStream_t stream);
 hipError_t launch_mx4_gated(p4q_dtype out_dt, Mx4Product p, hipStream_t stream);

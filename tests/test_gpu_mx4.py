@@ -268,7 +268,7 @@ def test_linear_row_gaps(M):
     N, K = 200, 288
     a, w = exact_operands(3, M, N, K)
     ref = store(oracle.mx4_linear(*a, *w)[0], "fp16")
-    for ld, first in ((N + 8, 0), (N + 3, 0), (N + 16, 2), (N + 24, 8)):
+    for ld, first in ((N + 8, 0), (N + 3, 0), (N + 16, 2), (N + 24, 8), (N + 24, 0), (N + 56, 32)):
         wide = torch.full((M, ld), 7.0, dtype=torch.float16, device=dev())
         p4q.mx4_linear(*gpu(a), *gpu(w), y=wide[:, first:first + N])
         assert np.array_equal(bits(to_np(wide[:, first:first + N].contiguous())), bits(ref)), (ld, first)
