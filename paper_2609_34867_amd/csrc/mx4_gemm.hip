@@ -742,7 +742,7 @@ hipError_t launch_typed(const Mx4Product &p, hipStream_t stream) {
     offer(22, 128, 2 * W, {0.55, 1.2, 1.5, 2});
     if (EPI == kLinear) offer(23, 128, 192, {0.7, 0.87, 2.3, 1});
     if (EPI == kLinear) offer(33, 192, 192, {0.85, 1.18, 2.8, 1});
-    offer(34, 192, 4 * W, {1.02, 1.42, 3.0, 1});
+    offer(34, 192, 4 * W, {1.02, 1.42, EPI == kLinear ? 2.2 : 2.7, 1});
     offer(44, 256, 4 * W, {1.18, 1.73, 4.0, 1});
     if constexpr (EPI == kLinear) {
         if (best == 11) return launch_tile<EPI, BF16, 1, 1, 4>(p, stream);
