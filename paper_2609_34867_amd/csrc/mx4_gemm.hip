@@ -669,8 +669,8 @@ __global__ __launch_bounds__(64 * NW) void k_mx4_rows(const Mx4Product p) {
 // to (15360, 5120) and gated (13824, 5120), where the kernel taken was within 3% of
 // the best one at most sizes and 8% behind it at worst.  For example N = 12288,
 // K = 4096: 64 rows 10.2 us by 64 x 64 tiles (16.4 as few rows, 13.1 by 128 x 128);
-// 384 rows 18.1 by 128 x 192 (20.1, 23.9 by 192 x 256); 704 rows 25.2 by 192 x 192
-// (31.6 by 128 x 128); 4096 rows 103.3 by 256 x 256 (123.9).
+// 384 rows 17.2 by 128 x 192 (19.9 by 128 x 128); 704 rows 23.3 by 192 x 192 (30.4 by
+// 128 x 128); 4096 rows 103.3 by 256 x 256 (123.9).
 struct TileCost {
     double idle, busy;                           // us a stage, of the first tile on the device and with every CU at work
     double epilogue;                             // us a round
