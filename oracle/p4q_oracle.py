@@ -1068,7 +1068,7 @@ def residual_rmsnorm(x, gamma, r=None, eps: float = 1e-5, dtype: str = "fp16", p
 
     def inverse(z):
         ms = np.mean(z * z, axis=1, keepdims=True) + eps
-        return np.where(ms > 0, 1.0 / np.sqrt(np.where(ms > 0, ms, 1.0)), 0.0)
+        return np.where(ms == 0, 0.0, 1.0 / np.sqrt(np.where(ms == 0, 1.0, ms)))
 
     h = x
     if r is not None:
