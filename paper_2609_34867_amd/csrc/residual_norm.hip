@@ -163,6 +163,7 @@ __global__ __launch_bounds__(NT) void k_residual_rmsnorm_quant(const ResidualNor
             }
             h[c] = round16x8<BF16>(o);
             if (q < chunks) store16(a.h_out + row * a.ldh, q, h[c]);
+            else h[c] = zero;                              // (0 times an infinity of post or gate is a NaN)
         }
     }
 
