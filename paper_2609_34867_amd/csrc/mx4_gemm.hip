@@ -46,9 +46,33 @@ __device__ __forceinline__ void mfma_mx4_16(v4i w, uint32_t sw, v4i a, uint32_t 
     acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(W, A, acc, 4, 4, I, (int)sw, I, (int)sa);
 }
 
-// (the hardware's exp2 and reciprocal, one unit in the last place each)
-__device__ __forceinline__ float silu(float g) {
-    return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896341f * g));
+// v = SiLU(v) u of N sums, v / (1 + 2^t) u with t = -v log2 e, by the hardware's exp2 and
+// reciprocal: one unit in the last place each where the reciprocal is a normal number, but
+// a subnormal one comes as 0, and u may bring the product back into range.  So below -87
+// u takes what SiLU(v) is of SiLU(-87), v / -87 2^(t(-87) - t), the power as a square since
+// it may pass the range before u does.  (u is used up.)  Whether any v is that low: as
+// whole numbers, the bits of negative ones rise with their magnitude and lie above those of
+// all others.
+template <int N>
+__device__ __forceinline__ void silu_mul(float (&v)[N], float (&u)[N]) {
+    constexpr float kLog2e = 1.44269504088896341f;
+    constexpr uint32_t kFar = 0xC2AE0000u;                 // -87
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) top = max(top, __float_as_uint(v[i]));
+    if (__builtin_expect(top > kFar, 0)) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if (__float_as_uint(v[i]) <= kFar) continue;
+            const float root = __builtin_amdgcn_exp2f(0.5f * __builtin_fmaf(kLog2e, v[i], 87.0f * kLog2e));
+            // (v of minus infinity: times 0, a NaN as its quotient)
+            u[i] = u[i] * root * root * (v[i] * (-1.0f / 87.0f));
+            v[i] = -87.0f;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        v[i] = v[i] * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * v[i])) * u[i];
 }
 
 // 8 consecutive 16-bit outputs n0 .. n0 + 7 of row m, as far as they exist
@@ -68,11 +92,8 @@ __device__ __forceinline__ void store8(const Mx4Product &p, int64_t m, int n0, u
 // 8 consecutive outputs n0 .. n0 + 7 of row m (u: the up sums, gated only).
 // Four lanes of a quad hold 32 outputs of one row in order.
 template <int EPI, bool BF16>
-__device__ __forceinline__ void emit8(const Mx4Product &p, int64_t m, int n0, float (&v)[8], const float (&u)[8]) {
-    if constexpr (EPI != kLinear) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = silu(v[i]) * u[i];
-    }
+__device__ __forceinline__ void emit8(const Mx4Product &p, int64_t m, int n0, float (&v)[8], float (&u)[8]) {
+    if constexpr (EPI != kLinear) silu_mul(v, u);
     if constexpr (EPI == kGatedQuant) {
         uint32_t byte;
         const uint32_t c = mx4_quantize(v, byte);
@@ -447,8 +468,7 @@ __global__ __launch_bounds__(256 * KS, FM * FN > 4 || RING > 2 || KS > 1 ? 1 : 2
                     if constexpr (EPI != kLinear) {
                         float u[16];
                         read_sums(acc[(f0 + e + FO) % FN][j], u);
-#pragma unroll
-                        for (int x = 0; x < 16; ++x) v[e][x] = silu(v[e][x]) * u[x];
+                        silu_mul(v[e], u);
                     }
                 }
                 if constexpr (EPI == kGatedQuant) {

@@ -7,7 +7,7 @@ import torch
 import oracle
 import paper_2609_34867_amd as p4q
 from gpu_util import Guarded, bits, check_canaries, dev, first_mismatch, to_gpu, to_np
-from test_gpu_mx4 import f64, rows, store
+from test_gpu_mx4 import HALF, TINY, TORCH, check_nearest, f64, gated_reference, gpu, rows, store
 
 pytestmark = pytest.mark.gpu
 
@@ -30,7 +30,7 @@ def test_norm_non_finite_vectors(d, dtype, bad, at, value):
     v[at] = value
     v = store(v, dtype)
     one = store(np.ones(d), dtype)
-    gh = Guarded((M, d), torch.float16 if dtype == "fp16" else torch.bfloat16, "h")
+    gh = Guarded((M, d), TORCH[dtype], "h")
     codes, scales, h = p4q.residual_rmsnorm_quant(to_gpu(x, dtype), to_gpu(one, dtype), to_gpu(r, dtype), h_out=gh.t,
                                                   **{bad: to_gpu(v, dtype)})
     torch.cuda.synchronize()
@@ -42,3 +42,47 @@ def test_norm_non_finite_vectors(d, dtype, bad, at, value):
     assert np.array_equal(got, ref, equal_nan=True)
     assert (m := first_mismatch(to_np(scales), rs)) is None, f"scales: {m}"
     assert (m := first_mismatch(to_np(codes), rc)) is None, f"codes: {m}"
+
+
+# --------------------------------------------------------------------------- gated products
+def far_gates(M, N, seed=0):
+    """Operands whose gates lie around -96 and -192, under up sums of any magnitude: exact
+    in fp32.  The first block of K = 64 makes the gate, the second the up sum."""
+    rng = np.random.default_rng(seed)
+    ac, sa = np.zeros((M, 32), np.uint8), np.zeros((M, 16), np.uint8)
+    wc, sw = np.zeros((2 * N, 32), np.uint8), np.zeros((2 * N, 16), np.uint8)
+    ac[:, :16], sa[:, 0] = 0x22, 127 + np.arange(M) % 2    # ones, or twos
+    ac[:, 16], sa[:, 1] = 0x02, 127
+    low = rng.integers(4, 7, (N, 16)) | 8                  # -2, -3, -4, sixteen of them
+    high = rng.integers(4, 7, (N, 16)) | 8
+    wc[:N, :16], sw[:N, 0] = low | (high << 4), 127
+    wc[N:, 16], sw[N:, 1] = rng.choice([2, 3, 5, 10], N), rng.integers(0, 254, N)
+    # (half of them near the top, where products come back into range)
+    sw[N:, 1][::2] = rng.integers(240, 254, (N + 1) // 2)
+    return (ac, sa), (wc, sw)
+
+
+# few rows (two and four wavefronts), and the tiles
+FAR = [(1, 512), (20, 512), (4, 16384), (130, 4000), (390, 4128), (700, 8224), (1300, 64), (4100, 2112)]
+
+
+@pytest.mark.parametrize("M,N", FAR)
+def test_gated_below_minus_87(M, N):
+    """Where 1 + exp(-gate) leaves the range that its reciprocal is held in, the product with
+    a large up sum is still a number of the output's range."""
+    a, w = far_gates(M, N)
+    K = 64
+    ref, tol = gated_reference(a, w, N, K, exact=True)
+    gate = oracle.mx4_linear(*a, w[0][:N], w[1][:N])[0]
+    assert (gate < -88).any() and (np.abs(ref)[gate < -88] > 1e-3).any()
+    # (and steps of the smallest fp32 number)
+    tol = tol + 2.0 ** -149
+    for dtype in ("bf16", "fp16"):
+        y = f64(to_np(p4q.mx4_gated_linear(*gpu(a), *gpu(w), out_dtype=TORCH[dtype])), dtype)
+        with np.errstate(over="ignore"):
+            top = f64(store(np.abs(ref) + tol, dtype), dtype)
+        lim = tol + HALF[dtype] * (np.abs(ref) + tol) + TINY[dtype]
+        ok = (np.abs(y - ref) <= lim) | (np.isinf(y) & np.isinf(top) & (np.sign(y) == np.sign(ref)))
+        assert ok.all(), f"{dtype}: {(~ok).sum()} values, first at {np.argwhere(~ok)[0]}"
+    codes, scales = p4q.mx4_gated_linear_quant(*gpu(a), *gpu(w))
+    check_nearest(to_np(codes), to_np(scales), ref, tol + np.abs(ref) * 2.0 ** -23 + 2.0 ** -150)
