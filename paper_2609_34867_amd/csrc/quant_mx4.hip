@@ -12,6 +12,8 @@
 #include "p4q_internal.h"
 #include "q4_device.h"
 
+#include <algorithm>
+
 namespace p4q {
 namespace {
 
@@ -23,7 +25,8 @@ __global__ __launch_bounds__(kThreads) void k_quant_mx4(const uint8_t *x, int64_
                                                         uint8_t *__restrict__ codes, uint8_t *__restrict__ scales,
                                                         uint8_t *values, int64_t ldv_bytes) {
     const int lane = threadIdx.x & 63;
-    const int64_t item = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
+    const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+    const int64_t item = block * (kThreads / 64) + (threadIdx.x >> 6);
     if (item >= items) return;
     const int64_t row = item / groups;
     const int q = (int)(item - row * groups) * 64 + lane;
@@ -54,10 +57,12 @@ hipError_t launch_quant_mx4(p4q_dtype dt, int M, int K, const void *x, int64_t l
                             uint8_t *scales, void *values, int64_t ldv, hipStream_t stream) {
     const int groups = (int)(mx4_scale_stride(K) / 16);
     const int64_t items = (int64_t)M * groups;
-    const unsigned blocks = (unsigned)((items + kThreads / 64 - 1) / (kThreads / 64));
+    // (a dimension of a grid holds less than 2^32 threads)
+    const unsigned blocks = (unsigned)((items + kThreads / 64 - 1) / (kThreads / 64)), most = 1u << 23;
+    const dim3 grid(std::min(blocks, most), (blocks + most - 1) / most);
     auto go = [&](auto kern) {
-        hipLaunchKernelGGL(kern, dim3(blocks), dim3(kThreads), 0, stream, static_cast<const uint8_t *>(x), ldx * 2,
-                           items, groups, K / 8, codes, scales, static_cast<uint8_t *>(values), ldv * 2);
+        hipLaunchKernelGGL(kern, grid, dim3(kThreads), 0, stream, static_cast<const uint8_t *>(x), ldx * 2, items, groups,
+                           K / 8, codes, scales, static_cast<uint8_t *>(values), ldv * 2);
         return hipGetLastError();
     };
     return dt == P4Q_BF16 ? go(k_quant_mx4<true>) : go(k_quant_mx4<false>);

@@ -86,3 +86,26 @@ def test_gated_below_minus_87(M, N):
         assert ok.all(), f"{dtype}: {(~ok).sum()} values, first at {np.argwhere(~ok)[0]}"
     codes, scales = p4q.mx4_gated_linear_quant(*gpu(a), *gpu(w))
     check_nearest(to_np(codes), to_np(scales), ref, tol + np.abs(ref) * 2.0 ** -23 + 2.0 ** -150)
+
+
+# --------------------------------------------------------------------------- quantizer
+@pytest.mark.parametrize("M", [(1 << 26) - 1, (1 << 25) + 5])
+def test_quant_most_rows(M):
+    """The largest calls that the limits admit (M ceil(K / 512) < 2^26): every row as in a
+    small call, and the row behind the last left as it was."""
+    K, n = 32, 4096
+    x = to_gpu(rows(5, n, K, "bf16"), "bf16")
+    rc, rs = p4q.quant_mx4(x)
+    big = -(-(M + 1) // n)
+    xs = x.repeat(big, 1)
+    codes = torch.full((big * n, K // 2), 9, dtype=torch.uint8, device=dev())
+    scales = torch.full((big * n, 16), 9, dtype=torch.uint8, device=dev())
+    p4q.quant_mx4(xs[:M], codes=codes[:M], scales=scales[:M])
+    torch.cuda.synchronize()
+    assert bool((codes[M:] == 9).all()) and bool((scales[M:] == 9).all())
+    whole = M // n * n
+    for got, ref in ((codes, rc), (scales, rs)):
+        for first in range(0, whole // n, 2048):
+            part = got.view(big, n, -1)[first:min(first + 2048, whole // n)]
+            assert bool((part == ref).all()), first
+        assert torch.equal(got[whole:M], ref[:M - whole])
