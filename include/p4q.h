@@ -548,7 +548,8 @@ int p4q_w4a4_linear(int M, int N_out, int K_in,
  * p4q_mx4_gated_linear_quant: the same, whose result leaves in MXFP4 instead
  *   (the codes of the fp32 products), ready for the next p4q_mx4_linear;
  *   N_out % 32 == 0.
- * The results of products must not overlap their operands.
+ * Results must not overlap each other nor, values in place apart, an operand;
+ *   calls whose operands do are refused.
  *
  * p4q_residual_rmsnorm_quant: what lies between two blocks of a decoder layer.
  *   r' = post_gamma ? r / rms(r) * post_gamma : r    (the block's output)
@@ -561,8 +562,8 @@ int p4q_w4a4_linear(int M, int N_out, int K_in,
  *   [M, ldh] (dt) receives h.  With r NULL, h = x, and h_out, gate and
  *   post_gamma must be NULL, alpha 1.  values, unless NULL: what the codes
  *   stand for, rounded to dt.  h_out may be x or r (same pointer and row
- *   stride); other overlaps are not allowed.  gamma, post_gamma and gate are
- *   [d] of dt.
+ *   stride); other overlaps with a result are refused.  gamma, post_gamma and
+ *   gate are [d] of dt.
  *
  * A row's results depend on that row alone (and, of products, on the weight, and
  *   in the last bits of the fp32 sums on M, whose size picks the kernel), not on

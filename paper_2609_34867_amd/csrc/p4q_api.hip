@@ -6,6 +6,7 @@
 #include <cstring>
 
 #include "kv_cache.h"
+#include "overlap.h"
 #include "p4q_internal.h"
 
 namespace {
@@ -532,6 +533,14 @@ size_t p4q_mx4_scale_stride(int K) {
     return (size_t)p4q::mx4_scale_stride(K);
 }
 
+using p4q::Rows;
+using p4q::rows_at;
+using p4q::share_memory;
+static Rows mx4_codes_at(const uint8_t *p, int64_t rows, int K) { return rows_at(p, rows, K / 2, K / 2); }
+static Rows mx4_scales_at(const uint8_t *p, int64_t rows, int K) {
+    return rows_at(p, rows, p4q::mx4_scale_stride(K), p4q::mx4_scale_stride(K));
+}
+
 // A 16-bit operand's rows: 16-byte aligned and at least `width` apart.
 static bool rows_ok(const void *p, int64_t ld, int width) { return aligned(p, 16) && ld >= width && ld % 8 == 0; }
 
@@ -549,6 +558,11 @@ int p4q_quant_mx4(p4q_dtype dt, int M, int K, const void *x, int64_t ldx, uint8_
     if (values == x && ldv != ldx)
         return fail(P4Q_ERR_INVALID_ARG, "p4q_quant_mx4: values in place need the same row stride");
     if (!aligned(codes, 16) || !aligned(scales, 16)) return fail(P4Q_ERR_INVALID_ARG, "p4q_quant_mx4: misaligned pointer");
+    const Rows in = rows_at(x, M, 2 * ldx, 2LL * K), held = rows_at(values, M, 2 * ldv, 2LL * K);
+    const Rows c = mx4_codes_at(codes, M, K), sc = mx4_scales_at(scales, M, K);
+    if ((values != x && share_memory(held, in)) || share_memory(c, sc) || share_memory(c, in) || share_memory(c, held) ||
+        share_memory(sc, in) || share_memory(sc, held))
+        return fail(P4Q_ERR_INVALID_ARG, "p4q_quant_mx4: operands overlap");
     return hip_status(p4q::launch_quant_mx4(dt, M, K, x, ldx, codes, scales, values, ldv, stream), "p4q_quant_mx4");
 }
 
@@ -571,6 +585,13 @@ static int check_mx4_output(const char *who, p4q_dtype out_dt, const void *y, in
     return P4Q_OK;
 }
 
+// `out`, a result, shares memory with an operand of the product (pair: rows of the weight for each output)
+static bool over_mx4_operand(const Rows &out, const p4q::Mx4Product &p, int pair) {
+    return share_memory(out, mx4_codes_at(p.a, p.M, p.K)) || share_memory(out, mx4_scales_at(p.as, p.M, p.K)) ||
+           share_memory(out, mx4_codes_at(p.w, (int64_t)pair * p.N, p.K)) ||
+           share_memory(out, mx4_scales_at(p.ws, (int64_t)pair * p.N, p.K));
+}
+
 static p4q::Mx4Product mx4_product(int M, int N_out, int K, const uint8_t *a_codes, const uint8_t *a_scales,
                                    const uint8_t *w_codes, const uint8_t *w_scales) {
     p4q::Mx4Product p = {};
@@ -587,6 +608,8 @@ int p4q_mx4_linear(int M, int N_out, int K, const uint8_t *a_codes, const uint8_
     if (const int st = check_mx4_output(who, out_dt, y, ldy, N_out)) return st;
     p4q::Mx4Product p = mx4_product(M, N_out, K, a_codes, a_scales, w_codes, w_scales);
     p.y = y, p.ldy = ldy;
+    if (over_mx4_operand(rows_at(y, M, 2 * ldy, 2LL * N_out), p, 1))
+        return fail(P4Q_ERR_INVALID_ARG, "%s: y overlaps an operand", who);
     return hip_status(p4q::launch_mx4_linear(out_dt, p, stream), who);
 }
 
@@ -598,6 +621,8 @@ int p4q_mx4_gated_linear(int M, int N_out, int K, const uint8_t *a_codes, const 
     if (const int st = check_mx4_output(who, out_dt, y, ldy, N_out)) return st;
     p4q::Mx4Product p = mx4_product(M, N_out, K, a_codes, a_scales, w_codes, w_scales);
     p.y = y, p.ldy = ldy;
+    if (over_mx4_operand(rows_at(y, M, 2 * ldy, 2LL * N_out), p, 2))
+        return fail(P4Q_ERR_INVALID_ARG, "%s: y overlaps an operand", who);
     return hip_status(p4q::launch_mx4_gated(out_dt, p, stream), who);
 }
 
@@ -614,6 +639,9 @@ int p4q_mx4_gated_linear_quant(int M, int N_out, int K, const uint8_t *a_codes,
         return fail(P4Q_ERR_INVALID_ARG, "%s: the result cannot replace the activations", who);
     p4q::Mx4Product p = mx4_product(M, N_out, K, a_codes, a_scales, w_codes, w_scales);
     p.codes = codes, p.scales = scales;
+    const Rows c = mx4_codes_at(codes, M, N_out), sc = mx4_scales_at(scales, M, N_out);
+    if (share_memory(c, sc) || over_mx4_operand(c, p, 2) || over_mx4_operand(sc, p, 2))
+        return fail(P4Q_ERR_INVALID_ARG, "%s: codes or scales overlap another operand", who);
     return hip_status(p4q::launch_mx4_gated(P4Q_BF16, p, stream), who);
 }
 
@@ -644,6 +672,18 @@ int p4q_residual_rmsnorm_quant(p4q_dtype dt, p4q_norm_format fmt, int M, int d, 
     if (!(alpha - alpha == 0.0f)) return fail(P4Q_ERR_INVALID_ARG, "%s: alpha %g", who, alpha);
     if (!valid_clip(clip) || (fmt == P4Q_NORM_MX4 && clip != 1.0f))
         return fail(P4Q_ERR_INVALID_ARG, "%s: clip %g (int4: in [2^-16, 1]; MXFP4: 1)", who, clip);
+    // h_out may be x or r; nothing else that is written shares memory
+    const Rows in[5] = {rows_at(x, M, 2 * ldx, 2LL * d), rows_at(r, M, 2 * ldr, 2LL * d), rows_at(gamma, 1, 2 * d, 2 * d),
+                        rows_at(post_gamma, 1, 2 * d, 2 * d), rows_at(gate, 1, 2 * d, 2 * d)};
+    const Rows out[4] = {rows_at(h_out, M, 2 * ldh, 2LL * d), rows_at(values, M, 2 * ldv, 2LL * d), mx4_codes_at(codes, M, d),
+                         fmt == P4Q_NORM_MX4 ? mx4_scales_at(static_cast<uint8_t *>(scales), M, d) : rows_at(scales, M, 4, 4)};
+    for (int i = 0; i < 4; ++i) {
+        for (int j = 0; j < i; ++j)
+            if (share_memory(out[i], out[j])) return fail(P4Q_ERR_INVALID_ARG, "%s: two results overlap", who);
+        for (int j = 0; j < 5; ++j)
+            if (share_memory(out[i], in[j]) && !(i == 0 && j < 2 && h_out == (j == 0 ? x : r)))
+                return fail(P4Q_ERR_INVALID_ARG, "%s: a result overlaps an operand (h_out may be x or r)", who);
+    }
     p4q::ResidualNorm a = {};
     a.M = M, a.d = d;
     a.x = static_cast<const uint16_t *>(x), a.ldx = ldx;

@@ -109,3 +109,43 @@ def test_quant_most_rows(M):
             part = got.view(big, n, -1)[first:min(first + 2048, whole // n)]
             assert bool((part == ref).all()), first
         assert torch.equal(got[whole:M], ref[:M - whole])
+
+
+# --------------------------------------------------------------------------- columns of one buffer
+def test_results_beside_their_operands():
+    """Columns of one wider buffer share no memory: x, r, h and values, and a product beside
+    rows that stay as they were."""
+    M, d = 37, 288
+    buf = torch.full((M, 4 * d), 7.0, dtype=torch.float16, device=dev())
+    x, r, h, v = (buf[:, i * d:(i + 1) * d] for i in range(4))
+    xs, rs = to_gpu(rows(1, M, d, "fp16", 1.0)), to_gpu(rows(2, M, d, "fp16", 1.0))
+    x.copy_(xs)
+    r.copy_(rs)
+    g = to_gpu(store(np.ones(d), "fp16"))
+    ref_v = torch.empty_like(xs)
+    ref = p4q.residual_rmsnorm_quant(xs, g, rs, values=ref_v)
+    got = p4q.residual_rmsnorm_quant(x, g, r, h_out=h, values=v)
+    assert all(torch.equal(a, b) for a, b in zip(got, ref)) and torch.equal(v, ref_v)
+    p4q.quant_mx4(x, values=v)
+    p4q.quant_mx4(xs, values=ref_v)
+    assert torch.equal(v, ref_v) and torch.equal(x, xs) and torch.equal(r, rs)
+    y = p4q.mx4_linear(*ref[:2], *p4q.quant_mx4(xs[:32]), out_dtype=torch.float16)
+    p4q.mx4_linear(*ref[:2], *p4q.quant_mx4(xs[:32]), y=h[:, :32])
+    assert torch.equal(h[:, :32], y) and torch.equal(x, xs) and torch.equal(v, ref_v)
+
+
+def test_overlapping_results_are_refused():
+    M, d = 8, 128
+    x, r, h = (torch.ones(M, d, dtype=torch.float16, device=dev()) for _ in range(3))
+    g = torch.ones(d, dtype=torch.float16, device=dev())
+    with pytest.raises(p4q.P4QError, match="results overlap"):
+        p4q.residual_rmsnorm_quant(x, g, r, h_out=h, values=h)
+    with pytest.raises(p4q.P4QError, match="overlaps an operand"):
+        p4q.residual_rmsnorm_quant(x, g, values=x)
+    codes, scales = p4q.quant_mx4(x)
+    w = p4q.quant_mx4(r)
+    for y in (codes.view(torch.float16), w[0].view(torch.float16)):
+        with pytest.raises(p4q.P4QError, match="y overlaps"):
+            p4q.mx4_linear(codes, scales, *w, y=y.view(-1)[:M * M].view(M, M))
+    torch.cuda.synchronize()
+    assert bool((x == 1).all()) and bool((h == 1).all()) and all(torch.equal(a, b) for a, b in zip((codes, scales), p4q.quant_mx4(x)))
