@@ -548,20 +548,23 @@ int p4q_w4a4_linear(int M, int N_out, int K_in,
  * p4q_mx4_gated_linear_quant: the same, whose result leaves in MXFP4 instead
  *   (the codes of the fp32 products), ready for the next p4q_mx4_linear;
  *   N_out % 32 == 0.
- * Results must not overlap each other nor, values in place apart, an operand;
- *   calls whose operands do are refused.
+ * Results must not overlap each other nor, values in place apart, an operand:
+ *   such calls are refused (of two operands with gaps between their rows and
+ *   different strides, where the first row of the one behind shows it).
  *
  * p4q_residual_rmsnorm_quant: what lies between two blocks of a decoder layer.
  *   r' = post_gamma ? r / rms(r) * post_gamma : r    (the block's output)
  *   h  = round(fl32(x + alpha * gate * r'))           (gate NULL: 1)
- *   P4Q_NORM_INT4: (codes, scales) = those of p4q_rmsnorm_quant(h, gamma, eps,
- *     clip): codes [M, d/2] of Q4, scales fp32 [M] (as there, for finite h gamma);
+ *   P4Q_NORM_INT4: codes [M, d/2] those of p4q_rmsnorm_quant(h, gamma, eps, clip),
+ *     scales fp32 [M] = fl32(Q4's scale / rms(h)) (there the rms is held in fp32,
+ *     so its scales agree to ~1e-6; as there, for finite h gamma);
  *   P4Q_NORM_MX4: (codes, scales) = MXFP4 of fl32(h * gamma / rms(h)),
  *   rms(z) = sqrt(sum z^2 / d + eps); a row with sum z^2 / d + eps = 0 counts as
  *   zeros.  Everything before a stated rounding is held in 64 bits.  h_out
  *   [M, ldh] (dt) receives h.  With r NULL, h = x, and h_out, gate and
  *   post_gamma must be NULL, alpha 1.  values, unless NULL: what the codes
- *   stand for, rounded to dt.  h_out may be x or r (same pointer and row
+ *   stand for, rounded to dt; of int4 the product of code and scale in fp32,
+ *   round(fl32(code * scale)).  h_out may be x or r (same pointer and row
  *   stride); other overlaps with a result are refused.  gamma, post_gamma and
  *   gate are [d] of dt.
  *

@@ -841,7 +841,8 @@ def residual_rmsnorm_quant(x: torch.Tensor, gamma: torch.Tensor, r: Optional[tor
 
     x, r [M, d] (row strides may exceed d); gamma, post_gamma and gate [d] of x's dtype.
     Returns (codes, scales, h); without r, h is x.  h_out may be x or r; `values`
-    [M, d], if given, receives what the codes stand for, rounded to x's dtype."""
+    [M, d], if given, receives what the codes stand for, rounded to x's dtype (int4:
+    code times scale in fp32 first)."""
     if x.dim() != 2:
         raise ValueError("x must be 2-D")
     mx4 = fmt == "mx4"

@@ -4,8 +4,9 @@
 //
 //   r' = post ? r / rms(r) * post : r
 //   h  = round16(fl32(x + alpha gate r'))            (no r: h = x)
-//   int4:  codes = Q4(u; clip), scale = fl32(s / rms(h)),  u = h gamma
-//   MXFP4: codes, scales of fl32(u / rms(h)), 32 values at a time
+//   int4:  codes = Q4(u; clip), scale = fl32(s / rms(h)),  u = h gamma;
+//          values round16(fl32(code scale))
+//   MXFP4: codes, scales of fl32(u / rms(h)), 32 values at a time; values exact in fp32
 //   rms(z) = sqrt(sum z^2 / d + eps)
 //
 // The sums of squares, their roots and what is multiplied by them are held in
@@ -225,6 +226,7 @@ __global__ __launch_bounds__(NT) void k_residual_rmsnorm_quant(const ResidualNor
             if (q < chunks) {
                 reinterpret_cast<uint32_t *>(a.codes)[row * chunks + q] = packed;
                 if (a.values) {
+                    // (in fp32 first, as the products' epilogue takes them)
                     float v[8];
 #pragma unroll
                     for (int k = 0; k < 8; ++k) v[k] = (float)((int)(packed << (28 - 4 * k)) >> 28) * scale;

@@ -149,3 +149,21 @@ def test_overlapping_results_are_refused():
             p4q.mx4_linear(codes, scales, *w, y=y.view(-1)[:M * M].view(M, M))
     torch.cuda.synchronize()
     assert bool((x == 1).all()) and bool((h == 1).all()) and all(torch.equal(a, b) for a, b in zip((codes, scales), p4q.quant_mx4(x)))
+
+
+# --------------------------------------------------------------------------- int4 values
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+def test_int4_values_round_in_fp32_first(dtype):
+    """values = round(fl32(code * scale)): at nearly a tie that differs from the product
+    rounded once, by one step."""
+    M, d = 20000, 512
+    x = rows(9, M, d, dtype, 1.0)
+    v = torch.empty(M, d, dtype=TORCH[dtype], device=dev())
+    codes, scales, _ = p4q.residual_rmsnorm_quant(to_gpu(x, dtype), to_gpu(store(np.ones(d), dtype), dtype), fmt="int4", values=v)
+    q, s = oracle.unpack_int4(to_np(codes)), to_np(scales)[:, None]
+    ref = store(q.astype(np.float32) * s, dtype)
+    assert (m := first_mismatch(bits(to_np(v)), bits(ref))) is None, m
+    if dtype == "fp16":
+        once = (q.astype(np.float64) * s.astype(np.float64)).astype(np.float16)
+        apart = np.abs(bits(once).astype(np.int64) - bits(ref).astype(np.int64))
+        assert apart.max() == 1
