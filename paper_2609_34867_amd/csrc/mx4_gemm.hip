@@ -14,6 +14,7 @@
 // sums of an output meet in one lane, and two lanes hold a block of 32 outputs
 // to quantize.
 #include "gemm_device.h"
+#include "mx4_choice.h"
 #include "mx4_device.h"
 #include "p4q_internal.h"
 
@@ -27,9 +28,6 @@ namespace {
 typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v16f __attribute__((ext_vector_type(16)));
-
-// what becomes of the sums
-enum Epilogue { kLinear, kGated, kGatedQuant };
 
 // acc += w a^T over 64 values of k (block I of each lane's four); sw, sa: the
 // words of scale bytes
@@ -681,41 +679,7 @@ __global__ __launch_bounds__(64 * NW) void k_mx4_rows(const Mx4Product p) {
     }
 }
 
-// ---- which kernel ------------------------------------------------------------------
-// Each kernel's time is estimated and the least taken.  What decides is how the
-// tiles fall into rounds and what a tile loads: one of 256 x 256 needs half of what
-// four of 128 x 128 load, and the last round may leave most CUs idle.  The numbers
-// are fitted to measurements on 256 CUs at M = 48 .. 11264 and (N, K) from (4096, 4096)
-// to (15360, 5120) and gated (13824, 5120), where the kernel taken was within 3% of
-// the best one at most sizes and 8% behind it at worst.  For example N = 12288,
-// K = 4096: 64 rows 10.2 us by 64 x 64 tiles (16.4 as few rows, 13.1 by 128 x 128);
-// 384 rows 17.2 by 128 x 192 (19.9 by 128 x 128); 704 rows 23.3 by 192 x 192 (30.4 by
-// 128 x 128); 4096 rows 103.3 by 256 x 256 (123.9).
-struct TileCost {
-    double idle, busy;                           // us a stage, of the first tile on the device and with every CU at work
-    double epilogue;                             // us a round
-    int per_cu;                                  // work-groups
-    int parts = 1;                               // that share k
-};
-inline double tile_cost(const Mx4Product &p, int bm, int bn, const TileCost &c, int cus) {
-    const int64_t tiles = (((int64_t)p.M + bm - 1) / bm) * (((int64_t)p.N + bn - 1) / bn);
-    const int64_t slots = (int64_t)cus * c.per_cu, whole = tiles / slots;
-    const int stages = ((p.K / 32 + 7) / 8 + c.parts - 1) / c.parts;
-    double us = 2.5 + (double)whole * (c.epilogue + stages * c.busy);
-    if (const int64_t left = tiles % slots) {
-        // two on a CU take nearly twice as long as one, whether or not every CU has two
-        const bool paired = left > cus;
-        us += c.epilogue + stages * (paired ? c.busy - 0.2 * (double)(slots - left) / cus
-                                            : c.idle + (c.busy / c.per_cu - c.idle) * (double)left / cus);
-    }
-    return us;
-}
-// the rows kernel: what its work-groups load, 15 MB a microsecond
-inline double rows_cost(const Mx4Product &p, int mb, int frags, int outputs) {
-    const double groups = ((p.N + outputs - 1) / outputs) * (double)((p.M + 16 * mb - 1) / (16 * mb));
-    return 3.5 + groups * ((p.K / 32 + 7) / 8) * (frags + mb) * 2176.0 / 15e6;
-}
-
+// ---- launches (mx4_choice.h has which) ---------------------------------------------
 // all outputs by tiles of 64 FM x 64 FN (gated: 32 FN)
 template <int EPI, bool BF16, int FM, int FN, int RING, int KS = 1>
 hipError_t launch_tile(const Mx4Product &p, hipStream_t stream) {
@@ -728,14 +692,11 @@ hipError_t launch_tile(const Mx4Product &p, hipStream_t stream) {
     return hipGetLastError();
 }
 
-// Two wavefronts a work-group where there are two for each CU or more, else four:
-// 32 rows at N = 12288, K = 4096 (768 work-groups) 6.7 against 9.4 us, one row at
-// N = 5120, K = 13824 (320) 11.1 against 8.2.
 template <int EPI, bool BF16, int MB>
 hipError_t launch_rows(const Mx4Product &p, int cus, hipStream_t stream) {
     constexpr int NO = EPI == kGatedQuant ? 32 : 16;
     const dim3 grid((unsigned)((p.N + NO - 1) / NO), (unsigned)((p.M + 16 * MB - 1) / (16 * MB)));
-    if ((int64_t)grid.x * grid.y >= 2 * cus)
+    if (mx4_rows_waves((int64_t)grid.x * grid.y, cus) == 2)
         hipLaunchKernelGGL((k_mx4_rows<EPI, BF16, MB, 2>), grid, dim3(128), 0, stream, p);
     else
         hipLaunchKernelGGL((k_mx4_rows<EPI, BF16, MB, 4>), grid, dim3(256), 0, stream, p);
@@ -744,38 +705,24 @@ hipError_t launch_rows(const Mx4Product &p, int cus, hipStream_t stream) {
 
 template <int EPI, bool BF16>
 hipError_t launch_typed(const Mx4Product &p, hipStream_t stream) {
-    constexpr int W = EPI == kLinear ? 64 : 32;            // outputs of 64 weight rows
-    constexpr int NO = EPI == kGatedQuant ? 32 : 16, F = EPI == kLinear ? 1 : EPI == kGated ? 2 : 4;
     const int cus = device_cus();
-    if (p.M <= 16) return launch_rows<EPI, BF16, 1>(p, cus, stream);
-    double least = p.M <= 1024 ? rows_cost(p, 2, F, NO) : 1e30;
-    int best = 0;
-    auto offer = [&](int which, int bm, int bn, const TileCost &c) {
-        const double us = tile_cost(p, bm, bn, c, cus);
-        if (us < least) least = us, best = which;
-    };
-    if (EPI == kLinear) offer(11, 64, 64, {0.38, 0.42, 1.0, 1});
-    if (EPI == kLinear) offer(112, 64, 64, {0.57, 0.70, 2.0, 1, 2});
-    if (EPI == kLinear) offer(122, 64, 128, {0.79, 0.86, 1.5, 1, 2});
-    if (EPI == kLinear) offer(12, 64, 128, {0.54, 0.95, 1.0, 2});
-    else offer(12, 64, 64, {0.5, 0.55, 1.0, 1});
-    offer(22, 128, 2 * W, {0.55, 1.2, 1.5, 2});
-    if (EPI == kLinear) offer(23, 128, 192, {0.7, 0.87, 2.3, 1});
-    if (EPI == kLinear) offer(33, 192, 192, {0.85, 1.18, 2.8, 1});
-    offer(34, 192, 4 * W, {1.02, 1.42, EPI == kLinear ? 2.2 : 2.7, 1});
-    offer(44, 256, 4 * W, {1.18, 1.73, 4.0, 1});
+    const Mx4Kernel which = mx4_kernel((Epilogue)EPI, p.M, p.N, p.K, cus);
     if constexpr (EPI == kLinear) {
-        if (best == 11) return launch_tile<EPI, BF16, 1, 1, 4>(p, stream);
-        if (best == 112) return launch_tile<EPI, BF16, 1, 1, 4, 2>(p, stream);
-        if (best == 122) return launch_tile<EPI, BF16, 1, 2, 2, 2>(p, stream);
-        if (best == 23) return launch_tile<EPI, BF16, 2, 3, 2>(p, stream);
-        if (best == 33) return launch_tile<EPI, BF16, 3, 3, 2>(p, stream);
+        switch (which) {
+            case kTile64x64: return launch_tile<EPI, BF16, 1, 1, 4>(p, stream);
+            case kTile64x64Parts: return launch_tile<EPI, BF16, 1, 1, 4, 2>(p, stream);
+            case kTile64x128Parts: return launch_tile<EPI, BF16, 1, 2, 2, 2>(p, stream);
+            case kTile128x192: return launch_tile<EPI, BF16, 2, 3, 2>(p, stream);
+            case kTile192x192: return launch_tile<EPI, BF16, 3, 3, 2>(p, stream);
+            default: break;
+        }
     }
-    switch (best) {
-        case 0: return launch_rows<EPI, BF16, 2>(p, cus, stream);
-        case 12: return launch_tile<EPI, BF16, 1, 2, EPI == kLinear ? 2 : 4>(p, stream);
-        case 22: return launch_tile<EPI, BF16, 2, 2, 2>(p, stream);
-        case 34: return launch_tile<EPI, BF16, 3, 4, 2>(p, stream);
+    switch (which) {
+        case kRows16: return launch_rows<EPI, BF16, 1>(p, cus, stream);
+        case kRows32: return launch_rows<EPI, BF16, 2>(p, cus, stream);
+        case kTile64x128: return launch_tile<EPI, BF16, 1, 2, EPI == kLinear ? 2 : 4>(p, stream);
+        case kTile128x128: return launch_tile<EPI, BF16, 2, 2, 2>(p, stream);
+        case kTile192x256: return launch_tile<EPI, BF16, 3, 4, 2>(p, stream);
         default: return launch_tile<EPI, BF16, 4, 4, 2>(p, stream);
     }
 }

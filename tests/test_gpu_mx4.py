@@ -229,7 +229,7 @@ SIZES = [(1, 1, 32), (1, 33, 64), (3, 5, 96), (16, 32, 256), (17, 31, 288), (31,
          (64, 256, 4096), (65, 129, 544), (128, 128, 1024), (130, 257, 1120), (257, 300, 320), (300, 520, 1568),
          (1, 4096, 4096), (5, 1000, 5120), (513, 768, 768), (1025, 1031, 1056), (2049, 2080, 512),
          (4100, 4200, 96), (3000, 6200, 1184), (16400, 1030, 288),
-         # where each size of tile is taken, with rows, columns and k past the last whole one
+         # several sizes of tile (mx4_sizes.py reaches each), with rows, columns and k past the last whole one
          (1300, 67, 96), (1290, 61, 1312), (130, 6211, 96), (4100, 1050, 800), (4090, 1056, 1056), (1300, 6211, 288),
          (1000, 8219, 96), (1000, 8224, 1056), (4100, 3003, 288), (4097, 3000, 1056),
          # where two parts of a work-group share k: the second with as many stages, with fewer
