@@ -197,6 +197,13 @@ __device__ __forceinline__ void add_parts(const Mx4Product &p, uint8_t *smem, in
     }
 }
 
+// What lanes of the wavefront stored to LDS before, its others read behind.  No instruction:
+// a wavefront's accesses of LDS keep their order, the compiler has to as well.
+__device__ __forceinline__ void lanes_meet() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 constexpr int kRowBytes = 128;                   // codes of a row in a stage
 constexpr int kRowScales = 16;                   // scale bytes of a row, two stages'
 
@@ -491,6 +498,7 @@ __global__ __launch_bounds__(256 * KS, FM * FN > 4 || RING > 2 || KS > 1 ? 1 : 2
                             *reinterpret_cast<uint2 *>(out + r * OUT_ROW + chunk * 16 + 8 * h) =
                                 make_uint2(round16x2<BF16>(o[0], o[1]), round16x2<BF16>(o[2], o[3]));
                         }
+                    lanes_meet();
                     constexpr int LR = 4 * EW;             // lanes per row
 #pragma unroll
                     for (int s = 0; s < 32 / (64 / LR); ++s) {
@@ -506,6 +514,7 @@ __global__ __launch_bounds__(256 * KS, FM * FN > 4 || RING > 2 || KS > 1 ? 1 : 2
                                                         reinterpret_cast<v4i *>(static_cast<uint16_t *>(p.y) + m * p.ldy + n));
                         else store8(p, m, n, val);
                     }
+                    lanes_meet();
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
