@@ -4,11 +4,14 @@
 // tiles fall into rounds and what a tile loads: one of 256 x 256 needs half of what
 // four of 128 x 128 load, and the last round may leave most CUs idle.  The numbers
 // are fitted to measurements on 256 CUs at M = 48 .. 11264 and (N, K) from (4096, 4096)
-// to (15360, 5120) and gated (13824, 5120), where the kernel taken was within 3% of
-// the best one at most sizes and 8% behind it at worst.  For example N = 12288,
-// K = 4096: 64 rows 10.2 us by 64 x 64 tiles (16.4 as few rows, 13.1 by 128 x 128);
-// 384 rows 17.2 by 128 x 192 (19.9 by 128 x 128); 704 rows 23.3 by 192 x 192 (30.4 by
-// 128 x 128); 4096 rows 103.3 by 256 x 256 (123.9).
+// to (15360, 5120) and gated (13824, 5120); they rank the kernels and are no forecast of
+// a call's time, where k is short least of all.  Every kernel timed at 24 .. 11264 rows of
+// the widths 1280 to 5120 (483 sizes): the one taken is within 3% of the best at 93% of
+// them, and at worst 29% behind it, in small linear products (256 x 2048 x 2048 7.2 us by
+// 64 x 64 tiles, 5.6 as few rows).
+// For example N = 12288, K = 4096: 64 rows 10.8 us by 64 x 64 tiles (13.1 as few rows,
+// 14.3 by 128 x 128); 384 rows 18.0 by 128 x 192 (20.6 by 128 x 128); 704 rows 24.8 by
+// 192 x 192 (31.9 by 128 x 128); 4096 rows 104 by 256 x 256 (125 by 128 x 128).
 #pragma once
 
 #include <stdint.h>
@@ -90,8 +93,10 @@ inline Mx4Kernel mx4_kernel(Epilogue form, int M, int N, int K, int cus) {
 }
 
 // Wavefronts of a few-rows work-group: two where there are two work-groups for each CU or
-// more, else four.  Linear, 32 rows at N = 12288, K = 4096 (768 work-groups) 6.7 against
-// 9.4 us, one row at N = 5120, K = 13824 (320) 11.1 against 8.2.
+// more, else four.  Linear, 32 rows at N = 12288, K = 4096 (768 work-groups) 7.4 against
+// 9.8 us, one row at N = 5120, K = 13824 (320) 11.5 against 8.5; gated, 16 rows at N =
+// 11008, K = 4096 (688) 9.7 against 12.1.  Gated and quantized, whose four take 100 KB of
+// LDS, two would be the better at N = 11008, K = 4096 (344) too: 10.4 against 11.9.
 inline int mx4_rows_waves(int64_t groups, int cus) { return groups >= 2 * cus ? 2 : 4; }
 
 }  // namespace p4q

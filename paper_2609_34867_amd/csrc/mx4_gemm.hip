@@ -110,15 +110,15 @@ __device__ __forceinline__ void emit8(const Mx4Product &p, int64_t m, int n0, fl
 // values, four steps each; a ring of RING stages in LDS is filled by DMA and runs
 // on across the tiles of a persistent work-group.
 //  * A stage's row is 128 bytes, one cache line, loaded by 8 lanes: rows of half a
-//    line (stages of 128 values, ring of 4) take 638 us where these take 502 (gate
-//    and up of 7B, 11264 rows).  Chunk c of 16 bytes (32 codes) of row r lies at
+//    line (stages of 128 values, ring of 4) took 638 us where these took 513 (gate
+//    and up of 7B, 11264 rows, before the next points).  Chunk c of 16 bytes (32 codes) of row r lies at
 //    c ^ (r / 2 % 8), so that 16 rows of a fragment read fall into distinct banks.
 //  * Scale bytes come 16 per row, for two stages at once (8 for one: 1024 instead
 //    of 768 lines a stage): the rows of a with the odd stage before, those of w
 //    with the even one.  An odd number of stages is padded with one that
 //    multiplies nothing.  (32 for four stages need the room that the outputs are
-//    staged in; stored from registers they take 243 us instead of 234, 7B down
-//    projection, 11264 rows.)
+//    staged in; stored from registers they took 243 us instead of 234 then, 7B
+//    down projection, 11264 rows.)
 //  * Operands are read ahead of their step: during steps 2 and 3 those of the next
 //    stage's steps 0 to 2, during step 0 those of step 3.  So a slot is read in
 //    three steps and has five for its next stage to arrive, whose DMAs are spread
@@ -127,16 +127,16 @@ __device__ __forceinline__ void emit8(const Mx4Product &p, int64_t m, int n0, fl
 //  * KS = 2: two parts of the work-group, of four wavefronts and a ring each, take a
 //    half of k each for the same tile, one tile per work-group, and add their sums in
 //    LDS.  For long rows and fewer tiles than CUs, where one wavefront per SIMD waits
-//    for its barriers and reads: 128 x 5120 x 13824 by 64 x 64 24.7 -> 20.6 us, 292 x
+//    for its barriers and reads, 128 x 5120 x 13824 by 64 x 64 24.7 -> 20.6 us, 292 x
 //    5120 x 13824 by 64 x 128 30.3 -> 26.1 (four parts no faster: 20.4).
 //  * Past the row's end the DMA's offsets lie outside the buffer and give codes
 //    of zero, and the scale bytes there are masked; rows past the last are outside
 //    it too.
 // Measured, M x N x K = 11264 x 4096 x 11008: 230 us = 4.4 PFLOP/s; gate and up,
-// 11264 x 2 * 11008 x 4096: 482 us = 4.2 PFLOP/s.  Of the 230 us the products alone
-// take 154, with their reads 177, and the DMA alone 133.  It is the power limit
-// that stretches them: the matrix units are busy in 55% of the cycles, at 1.84 GHz
-// of 2.4.
+// 11264 x 2 * 11008 x 4096: 495 us = 4.1 PFLOP/s.  Of the 230 us (237 when these were
+// taken) the products alone take 154, with their reads 177, and the DMA alone 133.  Much
+// of the rest is the power limit: the matrix units are busy in 55% of the cycles, at 1.83
+// GHz of 2.4, and alone on random codes they reach 6.6 PFLOP/s, on zeros 9.9.
 // The sums of a fragment out of the accumulation registers, here and not earlier (left
 // to itself the compiler reads them all before the first pass and spills).  It knows
 // no hazard of these reads: the caller keeps the distance to the last product.
@@ -538,8 +538,8 @@ __global__ __launch_bounds__(256 * KS, FM * FN > 4 || RING > 2 || KS > 1 ? 1 : 2
 //    In a product of 128 values lane l takes the blocks 2 (l / 16) and, in the
 //    second, 2 (l / 16) + 1 of row l % 16.
 //  * Scale bytes come 32 per row, for four stages at once, into two buffers.
-// Bound by memory: 13B down projection (N = 5120, K = 13824), 4 rows, 37.7 MB in 7.6
-// us = 5.0 TB/s; 7B gate and up, 16 rows, 48.3 MB in 9.2 us = 5.3 TB/s (12.4 and 16
+// Bound by memory: 13B down projection (N = 5120, K = 13824), 4 rows, 37.7 MB in 7.7
+// us = 4.9 TB/s; 7B gate and up, 16 rows, 48.3 MB in 9.2 us = 5.3 TB/s (12.4 and 16
 // with the operands straight from memory to registers: every fragment load touches
 // 32 lines there, and each line four times).
 constexpr int kRowsRing = 2, kRowsGroup = 4;

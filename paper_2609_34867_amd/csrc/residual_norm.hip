@@ -18,8 +18,10 @@
 // One work-group per row, which stays in registers from the load to the
 // codes: x and r are read once, h, the codes and the scales written once.  Bound by
 // memory where there are rows enough (11264 of 4096, MXFP4 with its values, 394 MB
-// in 60 us = 6.5 TB/s), else by the instructions of a row: 693 rows of 5120,
-// normalized before and after, int4 with its values, 11.5 us; one row of 4096 2.6 us.
+// in 69 us = 5.7 TB/s; 60 us again and again on the same rows).  693 rows of 5120,
+// normalized before and after, int4 with its values, 11.4 us: a wavefront's 1006 vector
+// instructions take about half of it on SIMDs that have three, its loads and two sums over
+// the row the rest.  One row of 4096 2.7 us.
 #include "mx4_device.h"
 #include "p4q_internal.h"
 #include "q4_device.h"
@@ -275,9 +277,9 @@ hipError_t launch_ch(p4q_norm_format fmt, const ResidualNorm &a, hipStream_t str
 }
 
 // 256 threads a row; where there is at most one row for each CU its latency counts,
-// and it gets a thread per 16 bytes, or per 32 (one row of 4096: 3.3 against 4.0 us;
-// 693 rows of 5120: 14.8 against 13.0).
-
+// and it gets a thread per 16 bytes, or per 32 (one row of 4096 2.75 against 2.9 us, 256
+// rows 3.6 against 3.8; 512 rows of 5120 7.3 against 6.25, 693 normalized before and after
+// 14.8 against 11.8).
 template <bool BF16>
 hipError_t launch_typed(p4q_norm_format fmt, const ResidualNorm &a, hipStream_t stream) {
     const int chunks = a.d / 8;                            // at most 2048
