@@ -111,8 +111,9 @@ __device__ __forceinline__ void emit8(const Mx4Product &p, int64_t m, int n0, fl
 // on across the tiles of a persistent work-group.
 //  * A stage's row is 128 bytes, one cache line, loaded by 8 lanes: rows of half a
 //    line (stages of 128 values, ring of 4) took 638 us where these took 513 (gate
-//    and up of 7B, 11264 rows, before the next points).  Chunk c of 16 bytes (32 codes) of row r lies at
-//    c ^ (r / 2 % 8), so that 16 rows of a fragment read fall into distinct banks.
+//    and up of 7B, 11264 rows, before the next points).  Chunk c of 16 bytes (32
+//    codes) of row r lies at c ^ (r / 2 % 8), so that 16 rows of a fragment read fall
+//    into distinct banks.
 //  * Scale bytes come 16 per row, for two stages at once (8 for one: 1024 instead
 //    of 768 lines a stage): the rows of a with the odd stage before, those of w
 //    with the even one.  An odd number of stages is padded with one that

@@ -536,6 +536,10 @@ size_t p4q_mx4_scale_stride(int K) {
 using p4q::Rows;
 using p4q::rows_at;
 using p4q::share_memory;
+// (a stride that no operand goes with may be any number)
+static Rows rows16_at(const void *p, int64_t rows, int64_t ld, int64_t cols) {
+    return p ? rows_at(p, rows, 2 * ld, 2 * cols) : Rows{};
+}
 static Rows mx4_codes_at(const uint8_t *p, int64_t rows, int K) { return rows_at(p, rows, K / 2, K / 2); }
 static Rows mx4_scales_at(const uint8_t *p, int64_t rows, int K) {
     return rows_at(p, rows, p4q::mx4_scale_stride(K), p4q::mx4_scale_stride(K));
@@ -558,7 +562,7 @@ int p4q_quant_mx4(p4q_dtype dt, int M, int K, const void *x, int64_t ldx, uint8_
     if (values == x && ldv != ldx)
         return fail(P4Q_ERR_INVALID_ARG, "p4q_quant_mx4: values in place need the same row stride");
     if (!aligned(codes, 16) || !aligned(scales, 16)) return fail(P4Q_ERR_INVALID_ARG, "p4q_quant_mx4: misaligned pointer");
-    const Rows in = rows_at(x, M, 2 * ldx, 2LL * K), held = rows_at(values, M, 2 * ldv, 2LL * K);
+    const Rows in = rows16_at(x, M, ldx, K), held = rows16_at(values, M, ldv, K);
     const Rows c = mx4_codes_at(codes, M, K), sc = mx4_scales_at(scales, M, K);
     if ((values != x && share_memory(held, in)) || share_memory(c, sc) || share_memory(c, in) || share_memory(c, held) ||
         share_memory(sc, in) || share_memory(sc, held))
@@ -608,7 +612,7 @@ int p4q_mx4_linear(int M, int N_out, int K, const uint8_t *a_codes, const uint8_
     if (const int st = check_mx4_output(who, out_dt, y, ldy, N_out)) return st;
     p4q::Mx4Product p = mx4_product(M, N_out, K, a_codes, a_scales, w_codes, w_scales);
     p.y = y, p.ldy = ldy;
-    if (over_mx4_operand(rows_at(y, M, 2 * ldy, 2LL * N_out), p, 1))
+    if (over_mx4_operand(rows16_at(y, M, ldy, N_out), p, 1))
         return fail(P4Q_ERR_INVALID_ARG, "%s: y overlaps an operand", who);
     return hip_status(p4q::launch_mx4_linear(out_dt, p, stream), who);
 }
@@ -621,7 +625,7 @@ int p4q_mx4_gated_linear(int M, int N_out, int K, const uint8_t *a_codes, const 
     if (const int st = check_mx4_output(who, out_dt, y, ldy, N_out)) return st;
     p4q::Mx4Product p = mx4_product(M, N_out, K, a_codes, a_scales, w_codes, w_scales);
     p.y = y, p.ldy = ldy;
-    if (over_mx4_operand(rows_at(y, M, 2 * ldy, 2LL * N_out), p, 2))
+    if (over_mx4_operand(rows16_at(y, M, ldy, N_out), p, 2))
         return fail(P4Q_ERR_INVALID_ARG, "%s: y overlaps an operand", who);
     return hip_status(p4q::launch_mx4_gated(out_dt, p, stream), who);
 }
@@ -673,9 +677,9 @@ int p4q_residual_rmsnorm_quant(p4q_dtype dt, p4q_norm_format fmt, int M, int d, 
     if (!valid_clip(clip) || (fmt == P4Q_NORM_MX4 && clip != 1.0f))
         return fail(P4Q_ERR_INVALID_ARG, "%s: clip %g (int4: in [2^-16, 1]; MXFP4: 1)", who, clip);
     // h_out may be x or r; nothing else that is written shares memory
-    const Rows in[5] = {rows_at(x, M, 2 * ldx, 2LL * d), rows_at(r, M, 2 * ldr, 2LL * d), rows_at(gamma, 1, 2 * d, 2 * d),
-                        rows_at(post_gamma, 1, 2 * d, 2 * d), rows_at(gate, 1, 2 * d, 2 * d)};
-    const Rows out[4] = {rows_at(h_out, M, 2 * ldh, 2LL * d), rows_at(values, M, 2 * ldv, 2LL * d), mx4_codes_at(codes, M, d),
+    const Rows in[5] = {rows16_at(x, M, ldx, d), rows16_at(r, M, ldr, d), rows16_at(gamma, 1, d, d),
+                        rows16_at(post_gamma, 1, d, d), rows16_at(gate, 1, d, d)};
+    const Rows out[4] = {rows16_at(h_out, M, ldh, d), rows16_at(values, M, ldv, d), mx4_codes_at(codes, M, d),
                          fmt == P4Q_NORM_MX4 ? mx4_scales_at(static_cast<uint8_t *>(scales), M, d) : rows_at(scales, M, 4, 4)};
     for (int i = 0; i < 4; ++i) {
         for (int j = 0; j < i; ++j)

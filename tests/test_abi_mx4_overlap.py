@@ -41,7 +41,8 @@ def refused(fn, **kw):
 
 @pytest.mark.parametrize("kw", [
     dict(values=S + ROW), dict(values=S - ROW), dict(values=S + 2 * 32), dict(codes=S), dict(codes=S + 3 * ROW), dict(scales=S),
-    dict(codes=4 * S), dict(scales=4 * S + 3 * ROW), dict(scales=2 * S), dict(scales=2 * S + 4 * 32 - 16), dict(codes=3 * S + 4 * 16 - 16)])
+    dict(codes=4 * S), dict(scales=4 * S + 3 * ROW), dict(scales=2 * S), dict(scales=2 * S + 4 * 32 - 16), dict(codes=3 * S + 4 * 16 - 16),
+    dict(values=None, ldv=2 ** 63 - 1, codes=S)])
 def test_quantizer(kw):
     refused("p4q_quant_mx4", **kw)
 
@@ -72,6 +73,7 @@ def test_quantized_product_results():
     dict(h=S + ROW), dict(h=2 * S + 2 * 32), dict(h=3 * S), dict(h=5 * S + 64), dict(codes=6 * S), dict(codes=S), dict(codes=8 * S),
     dict(scales=9 * S), dict(scales=3 * S), dict(scales=7 * S + 16), dict(fmt=0, scales=6 * S), dict(fmt=0, scales=7 * S + 124),
     # without a residual x is the result
-    dict(r=None, h=None, post=None, gate=None, values=S)])
+    dict(r=None, h=None, post=None, gate=None, values=S),
+    dict(r=None, ldr=2 ** 63 - 1, h=None, ldh=-2 ** 63, post=None, gate=None, values=S)])
 def test_norm(kw):
     refused("p4q_residual_rmsnorm_quant", **kw)
